@@ -8,6 +8,8 @@
  *   - the fused 8-bit Adam / AdamW / Momentum / AdaGrad step (Section 3, Eq. 1-2, App. H),
  *     and LAMB / LARS through step plans (App. E)
  *   - the quantile maps and their GPU estimator                 (App. F.2, App. G)
+ * and the operators that run around that step in a training program: layer norm,
+ * embedding lookup, the stable embedding layer (Section 3.3), gradient clipping.
  *
  * Conventions shared by every call
  *   - Pointers named "device" must point to GPU memory of the current HIP
@@ -436,6 +438,179 @@ bq_status bq_step_plan_run_device(bq_step_plan plan, bq_hparams *hp_device, int3
 
 /* Free a plan's device memory (synchronizes with the device).  NULL is a no-op. */
 bq_status bq_step_plan_destroy(bq_step_plan plan);
+
+/* ------------------------------------------------------------------------
+ * Operators around the optimizer step: layer norm, embedding lookup, the stable
+ * embedding layer (Section 3.3), and the norm of a gradient list with clipping.
+ *
+ * Element arrays of these calls need the alignment of their elements only, and
+ * rows may have any length.  Arithmetic is fp32 (the gradient norm's sums:
+ * fp64), each result rounded once where it is stored; sums have a fixed order,
+ * so a call gives the same bits every time.  Outputs must not overlap inputs.
+ * Non-finite inputs follow IEEE arithmetic: a row or sum that holds one is
+ * not finite.  A workspace belongs to one call until that call has run: calls
+ * that may overlap (on two streams, or in two captured graphs) need one each.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Layer norm of rows of cols values: with mean and var (over cols, biased) of a
+ * row, rstd = 1 / sqrt(var + eps) and xh = (x - mean) rstd,
+ *   y = xh * weight + bias.
+ *   dtype        of x and y; param_dtype of weight and bias: dtype or BQ_F32
+ *   x            device, rows rows, row_stride elements apart (0: one row for all)
+ *   weight, bias device, cols elements each; NULL: ones, zeros
+ *   y            device, rows x cols, packed (written)
+ *   mean, rstd   device, rows fp32 each (written), both or neither NULL
+ * Errors: BQ_ERR_DTYPE, BQ_ERR_SIZE (rows < 0, cols < 1, row_stride < 0, or too
+ * large), BQ_ERR_ARG (eps negative or not finite), BQ_ERR_NULL, BQ_ERR_ALIGN,
+ * BQ_ERR_HIP.
+ */
+bq_status bq_layer_norm_forward(bq_dtype dtype, bq_dtype param_dtype, const void *x, int64_t rows,
+                                int64_t cols, int64_t row_stride, const void *weight,
+                                const void *bias, float eps, void *y, float *mean, float *rstd,
+                                hipStream_t stream);
+
+/* Bytes of device workspace of bq_layer_norm_backward where it is asked for
+ * dweight or dbias (0 for sizes that the call refuses). */
+int64_t bq_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * Gradients of the layer norm: with g = dy * weight,
+ *   dx = rstd (g - mean(g) - xh mean(g xh)),
+ *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
+ *   dy, x      device, rows rows, dy_stride and x_stride elements apart
+ *   mean, rstd device, rows fp32 each, as bq_layer_norm_forward wrote them
+ *   dx         device, rows x cols, packed (written), or NULL
+ *   dweight, dbias  device, cols elements of param_dtype each (written; zeros
+ *              where rows == 0), each may be NULL
+ *   workspace  device, bq_layer_norm_workspace_bytes(rows, cols), 16-byte
+ *              aligned; may be NULL where dweight and dbias are
+ * Errors: as bq_layer_norm_forward.
+ */
+bq_status bq_layer_norm_backward(bq_dtype dtype, bq_dtype param_dtype, const void *dy,
+                                 int64_t dy_stride, const void *x, int64_t x_stride, int64_t rows,
+                                 int64_t cols, const void *weight, const float *mean,
+                                 const float *rstd, void *dx, void *dweight, void *dbias,
+                                 void *workspace, hipStream_t stream);
+
+/*
+ * Embedding lookup with scaling: out[i] = scale * weight[ids[i]].
+ *   dtype, out_dtype  of weight and out: the same, or weight BQ_F32
+ *   weight   device, num x dim
+ *   ids      device, count integers of id_bits (32 or 64) bits; an id outside
+ *            [0, num) reads nothing and gives a row of NaN
+ *   out      device, count x dim (written)
+ * Errors: BQ_ERR_DTYPE (types, id_bits), BQ_ERR_SIZE (count < 0 or >= 2^31,
+ * num < 1 or >= 2^31 - 1, dim < 1 or > 2^30), BQ_ERR_ARG (scale not finite),
+ * BQ_ERR_NULL, BQ_ERR_ALIGN, BQ_ERR_HIP.
+ */
+bq_status bq_embedding_forward(bq_dtype dtype, bq_dtype out_dtype, const void *weight, int64_t num,
+                               int64_t dim, const void *ids, int32_t id_bits, int64_t count,
+                               float scale, void *out, hipStream_t stream);
+
+/* Bytes of device workspace of bq_embedding_backward (0 for sizes that it refuses). */
+int64_t bq_embedding_workspace_bytes(int64_t count, int64_t num, int64_t dim);
+
+/*
+ * Gradient of the lookup, dense: dweight[v] = scale * sum of dout[i] over the i
+ * with ids[i] == v, in the order of i (tokens are sorted by id, and long runs of
+ * one id summed in fixed parts); zeros for rows without tokens and for the row
+ * `padding` (-1: none).  Ids outside [0, num) are left out.
+ *   dout       device, count x dim of out_dtype
+ *   dweight    device, num x dim of dtype (every element written)
+ *   workspace  device, bq_embedding_workspace_bytes(count, num, dim), 16-byte
+ *              aligned (may be NULL where count == 0)
+ * Errors: as bq_embedding_forward; BQ_ERR_ARG for padding outside [-1, num).
+ */
+bq_status bq_embedding_backward(bq_dtype dtype, bq_dtype out_dtype, const void *dout,
+                                const void *ids, int32_t id_bits, int64_t count, int64_t num,
+                                int64_t dim, int64_t padding, float scale, void *dweight,
+                                void *workspace, hipStream_t stream);
+
+/* The longest row of the stable embedding's calls. */
+#define BQ_STABLE_EMBEDDING_MAX_DIM 16384
+
+/*
+ * The stable embedding layer of Section 3.3 as one operator: the layer norm of
+ * the looked-up row, out[i] = layer_norm(weight[ids[i]]), without the looked-up
+ * rows in memory.
+ *   norm_weight, norm_bias  device, dim elements of dtype each; NULL: ones, zeros
+ * The other arguments as bq_embedding_forward and bq_layer_norm_forward.
+ * Errors: as those; BQ_ERR_SIZE for dim > BQ_STABLE_EMBEDDING_MAX_DIM.
+ */
+bq_status bq_stable_embedding_forward(bq_dtype dtype, bq_dtype out_dtype, const void *weight,
+                                      int64_t num, int64_t dim, const void *ids, int32_t id_bits,
+                                      int64_t count, const void *norm_weight,
+                                      const void *norm_bias, float eps, void *out,
+                                      hipStream_t stream);
+
+/* Bytes of device workspace of bq_stable_embedding_backward (0 for sizes that it
+ * refuses). */
+int64_t bq_stable_embedding_workspace_bytes(int64_t count, int64_t num, int64_t dim);
+
+/*
+ * Gradients of the stable embedding.  Every token of a row looks up the same
+ * values, so with S_v the sum of dout over the row's tokens and G = S_v *
+ * norm_weight: dweight[v] = rstd_v (G - mean(G) - xh_v mean(G xh_v)),
+ * dnorm_weight = sum over v of S_v xh_v, dnorm_bias = sum over v of S_v.  The row
+ * `padding` (-1: none) gets a zero dweight; its tokens count in the other two.
+ *   weight      device, num x dim, the table of the forward pass
+ *   dweight     device, num x dim (every element written)
+ *   dnorm_weight, dnorm_bias  device, dim elements each (written), may be NULL
+ *   workspace   device, bq_stable_embedding_workspace_bytes(count, num, dim),
+ *               16-byte aligned
+ * Errors: as bq_stable_embedding_forward and bq_embedding_backward.
+ */
+bq_status bq_stable_embedding_backward(bq_dtype dtype, bq_dtype out_dtype, const void *dout,
+                                       const void *ids, int32_t id_bits, int64_t count,
+                                       const void *weight, int64_t num, int64_t dim,
+                                       int64_t padding, const void *norm_weight, float eps,
+                                       void *dweight, void *dnorm_weight, void *dnorm_bias,
+                                       void *workspace, hipStream_t stream);
+
+typedef enum bq_norm {
+    BQ_NORM_L2 = 0,
+    BQ_NORM_INF = 1,
+    /* not values: these two make the type span every int, so a call that
+     * receives any int in it has defined behavior (and rejects it) */
+    BQ_NORM_RANGE_MIN = -2147483647 - 1,
+    BQ_NORM_RANGE_MAX = 2147483647
+} bq_norm;
+
+/* One gradient of a list: numel elements of dtype in device memory. */
+typedef struct bq_grad {
+    void *data;
+    int64_t numel;
+    bq_dtype dtype;
+} bq_grad;
+
+/* Bytes of device workspace of the two calls below for ngrads gradients. */
+int64_t bq_grad_norm_workspace_bytes(int32_t ngrads);
+
+/*
+ * The norm of a list of gradients taken as one vector: the root of the sum of
+ * squares (BQ_NORM_L2, summed in fp64) or the largest magnitude (BQ_NORM_INF);
+ * 0 for an empty list.
+ *   grads      host array of ngrads descriptors (types may differ)
+ *   workspace  device, bq_grad_norm_workspace_bytes(ngrads), 8-byte aligned
+ *   norm       device, one fp32 (written)
+ * Errors: BQ_ERR_ENUM, BQ_ERR_SIZE (ngrads or a numel negative, or more than 2^30
+ * tiles of 16 KiB), BQ_ERR_NULL, BQ_ERR_DTYPE, BQ_ERR_ALIGN, BQ_ERR_HIP.
+ */
+bq_status bq_grad_norm(const bq_grad *grads, int32_t ngrads, bq_norm kind, void *workspace,
+                       float *norm, hipStream_t stream);
+
+/*
+ * The norm as above, then every gradient in place times
+ *   c = min(1, max_norm / (norm + 1e-6)),
+ * formed in fp64 and rounded to fp32; each product is rounded once to the
+ * gradient's type.  Where c is 1 the gradients are left as they are.  A norm
+ * that is infinite makes c 0, a NaN makes it NaN, as IEEE arithmetic has it.
+ * The host reads nothing: the call can be captured into a graph.
+ * Errors: as bq_grad_norm; BQ_ERR_ARG (max_norm negative or NaN).
+ */
+bq_status bq_clip_grad_norm(const bq_grad *grads, int32_t ngrads, bq_norm kind, double max_norm,
+                            void *workspace, float *norm, hipStream_t stream);
 
 /* Static, human-readable name of a status code (never NULL). */
 const char *bq_status_string(bq_status s);

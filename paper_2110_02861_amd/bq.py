@@ -39,9 +39,16 @@ EXPORTS = ("bq_make_dynamic_codebook", "bq_make_codebook", "bq_make_quantile_cod
            "bq_prepare_codebook",
            "bq_quantize_blockwise_prepared",
            "bq_step_plan_create", "bq_step_plan_run", "bq_step_plan_run_prepared",
-           "bq_step_plan_run_device", "bq_step_plan_destroy", "bq_status_string")
+           "bq_step_plan_run_device", "bq_step_plan_destroy", "bq_status_string",
+           "bq_layer_norm_forward", "bq_layer_norm_workspace_bytes", "bq_layer_norm_backward",
+           "bq_embedding_forward", "bq_embedding_workspace_bytes", "bq_embedding_backward",
+           "bq_stable_embedding_forward", "bq_stable_embedding_workspace_bytes",
+           "bq_stable_embedding_backward", "bq_grad_norm_workspace_bytes", "bq_grad_norm",
+           "bq_clip_grad_norm")
 BQ_PREPARED_CODEBOOK_BYTES = 8720
 BQ_QUANTILE_CHUNK = 4096
+BQ_NORM_L2, BQ_NORM_INF = 0, 1
+BQ_STABLE_EMBEDDING_MAX_DIM = 16384
 
 
 class BQError(RuntimeError):
@@ -67,6 +74,10 @@ class bq_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float),
                 ("step", ctypes.c_int64), ("trust_coeff", ctypes.c_float)]
+
+
+class bq_grad(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int)]
 
 
 _lib = None
@@ -115,6 +126,28 @@ def lib() -> ctypes.CDLL:
         L.bq_step_plan_run_device.restype = I
         L.bq_step_plan_destroy.argtypes = [P]
         L.bq_step_plan_destroy.restype = I
+        F, D = ctypes.c_float, ctypes.c_double
+        L.bq_layer_norm_forward.argtypes = [I, I, P, I64, I64, I64, P, P, F, P, P, P, P]
+        L.bq_layer_norm_workspace_bytes.argtypes = [I64, I64]
+        L.bq_layer_norm_backward.argtypes = [I, I, P, I64, P, I64, I64, I64, P, P, P, P, P, P, P,
+                                             P]
+        L.bq_embedding_forward.argtypes = [I, I, P, I64, I64, P, I32, I64, F, P, P]
+        L.bq_embedding_workspace_bytes.argtypes = [I64, I64, I64]
+        L.bq_embedding_backward.argtypes = [I, I, P, P, I32, I64, I64, I64, I64, F, P, P, P]
+        L.bq_stable_embedding_forward.argtypes = [I, I, P, I64, I64, P, I32, I64, P, P, F, P, P]
+        L.bq_stable_embedding_workspace_bytes.argtypes = [I64, I64, I64]
+        L.bq_stable_embedding_backward.argtypes = [I, I, P, P, I32, I64, P, I64, I64, I64, P, F, P,
+                                                   P, P, P, P]
+        L.bq_grad_norm_workspace_bytes.argtypes = [I32]
+        L.bq_grad_norm.argtypes = [P, I32, I, P, P, P]
+        L.bq_clip_grad_norm.argtypes = [P, I32, I, D, P, P, P]
+        for name in ("bq_layer_norm", "bq_embedding", "bq_stable_embedding"):
+            getattr(L, name + "_forward").restype = I
+            getattr(L, name + "_backward").restype = I
+            getattr(L, name + "_workspace_bytes").restype = I64
+        L.bq_grad_norm_workspace_bytes.restype = I64
+        L.bq_grad_norm.restype = I
+        L.bq_clip_grad_norm.restype = I
         L.bq_status_string.argtypes = [I]
         L.bq_status_string.restype = ctypes.c_char_p
         _lib = L
@@ -604,3 +637,349 @@ def read_device_hparams(t) -> dict:
 
 def bq_step_plan_destroy(plan: StepPlan):
     plan.close()
+
+
+# ---------------------------------------------------------------------------
+# Operators around the optimizer step
+# ---------------------------------------------------------------------------
+
+def _dtype_id(t, name):
+    import torch
+    d = {torch.float32: BQ_F32, torch.float16: BQ_F16, torch.bfloat16: BQ_BF16}.get(
+        t if isinstance(t, torch.dtype) else getattr(t, "dtype", None))
+    if d is None:
+        raise TypeError(f"{name} must be fp32, fp16 or bf16")
+    return d
+
+
+def _on_device(t, name):
+    """t, a dense GPU tensor on the current device."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided:
+        raise TypeError(f"{name} must be a dense GPU torch tensor")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return t
+
+
+def _rows_of(t, name):
+    """(rows, cols, elements between rows) of a GPU tensor whose last dimension is packed."""
+    _on_device(t, name)
+    if t.dim() == 0 or t.size(-1) == 0:
+        raise ValueError(f"{name} needs a last dimension of at least one element")
+    cols = t.size(-1)
+    if t.is_contiguous():
+        return t.numel() // cols, cols, cols
+    if t.dim() == 2 and (t.stride(1) == 1 or cols == 1):
+        return t.size(0), cols, t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or two-dimensional with packed rows")
+
+
+def _vector(t, n, dtype, name):
+    """Pointer of an optional parameter vector of n elements of dtype."""
+    if t is None:
+        return None
+    _on_device(t, name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous elements")
+    return t.data_ptr()
+
+
+def _other(stream):
+    """stream, where it is not the current one; else None."""
+    import torch
+    return None if stream is None or stream == torch.cuda.current_stream() else stream
+
+
+def _empty(shape, dtype, device, other):
+    """A buffer for a call on stream `other` (None: the current one): it comes from that
+    stream's memory, and is not given away while the current stream may use it."""
+    import torch
+    if other is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(other):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _output(out, shape, dtype, device, other, name):
+    if out is None:
+        return _empty(shape, dtype, device, other)
+    _on_device(out, name)
+    if out.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
+    if tuple(out.shape) != tuple(shape) or not out.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of shape {tuple(shape)}")
+    return out
+
+
+def _workspace(workspace, nbytes, device, other):
+    """A device buffer of at least nbytes."""
+    import torch
+    if workspace is None:
+        return _empty((max(16, nbytes),), torch.uint8, device, other)
+    _on_device(workspace, "workspace")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    if workspace.numel() * workspace.element_size() < nbytes:
+        raise ValueError(f"workspace holds {workspace.numel() * workspace.element_size()} bytes, "
+                         f"needs {nbytes}")
+    return workspace
+
+
+def _norm_params(x, weight, bias, cols):
+    """(dtype of the parameters, pointer of weight, pointer of bias) of a layer norm."""
+    import torch
+    given = weight if weight is not None else bias
+    dtype = x.dtype if given is None else given.dtype
+    if dtype not in (torch.float32, x.dtype):
+        raise TypeError(f"weight and bias must be fp32 or {x.dtype}, got {dtype}")
+    return dtype, _vector(weight, cols, dtype, "weight"), _vector(bias, cols, dtype, "bias")
+
+
+def bq_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, stats: bool = False,
+                          out=None, stream=None):
+    """The layer norm of x over its last dimension; with stats, (y, mean, rstd), the
+    fp32 statistics of every row that the backward pass takes.  weight and bias: of
+    x's type or fp32, both alike, each may be None."""
+    import torch
+    rows, cols, stride = _rows_of(x, "x")
+    xt = _dtype_id(x, "x")
+    pdtype, w, b = _norm_params(x, weight, bias, cols)
+    other = _other(stream)
+    y = _output(out, x.shape, x.dtype, x.device, other, "out")
+    mean = rstd = None
+    if stats:
+        mean = _empty((rows,), torch.float32, x.device, other)
+        rstd = _empty((rows,), torch.float32, x.device, other)
+    _check(lib().bq_layer_norm_forward(xt, _dtype_id(pdtype, "weight"), x.data_ptr(), rows, cols,
+                                       stride, w, b, eps, y.data_ptr(),
+                                       mean.data_ptr() if stats else None,
+                                       rstd.data_ptr() if stats else None, _stream(stream)),
+           "bq_layer_norm_forward")
+    return (y, mean, rstd) if stats else y
+
+
+def bq_layer_norm_backward(dy, x, weight, mean, rstd, need_dx: bool = True,
+                           need_params: bool = True, param_dtype=None, workspace=None,
+                           stream=None):
+    """(dx, dweight, dbias) of the layer norm of x, None where not needed; mean and rstd as
+    bq_layer_norm_forward returned them.  The parameters' gradients have weight's type
+    (param_dtype where weight is None)."""
+    import torch
+    rows, cols, stride = _rows_of(x, "x")
+    xt = _dtype_id(x, "x")
+    if not isinstance(dy, torch.Tensor) or dy.dtype != x.dtype or dy.shape != x.shape:
+        raise TypeError("dy must have x's type and shape")
+    _, _, dy_stride = _rows_of(dy, "dy")
+    if weight is None and param_dtype is not None:
+        if param_dtype not in (torch.float32, x.dtype):
+            raise TypeError(f"param_dtype must be fp32 or {x.dtype}")
+        pdtype, w = param_dtype, None
+    else:
+        pdtype, w, _ = _norm_params(x, weight, None, cols)
+    m, r = (_vector(t, rows, torch.float32, n) for t, n in ((mean, "mean"), (rstd, "rstd")))
+    if m is None or r is None:
+        raise TypeError("mean and rstd are required")
+    other = _other(stream)
+    dx = _empty(x.shape, x.dtype, x.device, other) if need_dx else None
+    dw = db = ws = None
+    if need_params:
+        dw = _empty((cols,), pdtype, x.device, other)
+        db = _empty((cols,), pdtype, x.device, other)
+        ws = _workspace(workspace, lib().bq_layer_norm_workspace_bytes(rows, cols), x.device, other)
+    _check(lib().bq_layer_norm_backward(
+        xt, _dtype_id(pdtype, "weight"), dy.data_ptr(), dy_stride, x.data_ptr(), stride, rows, cols,
+        w, m, r, *(None if t is None else t.data_ptr() for t in (dx, dw, db, ws)),
+        _stream(stream)), "bq_layer_norm_backward")
+    return dx, dw, db
+
+
+def _ids_of(ids):
+    """(pointer, bits) of a GPU tensor of token ids."""
+    import torch
+    _on_device(ids, "ids")
+    if ids.dtype not in (torch.int64, torch.int32):
+        raise TypeError(f"ids must be int64 or int32, got {ids.dtype}")
+    if not ids.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return ids.data_ptr(), 64 if ids.dtype == torch.int64 else 32
+
+
+def _table_of(weight):
+    """(dtype id, rows, dim) of an embedding table."""
+    _on_device(weight, "weight")
+    if weight.dim() != 2 or not weight.is_contiguous():
+        raise ValueError("weight must be a contiguous matrix")
+    return _dtype_id(weight, "weight"), weight.size(0), weight.size(1)
+
+
+def _lookup_dtype(weight_dtype, out_dtype):
+    import torch
+    out = weight_dtype if out_dtype is None else out_dtype
+    _dtype_id(out, "out_dtype")
+    if weight_dtype not in (torch.float32, out):
+        raise TypeError(f"a {weight_dtype} table gives {weight_dtype} rows, not {out}")
+    return out
+
+
+def _padding(padding_idx, num):
+    """padding_idx as a row (negative ones count from the end), -1 for None."""
+    if padding_idx is None:
+        return -1
+    if not -num <= padding_idx < num:
+        raise ValueError(f"padding_idx {padding_idx} is outside of a table of {num} rows")
+    return padding_idx % num
+
+
+def bq_embedding_forward(weight, ids, scale: float = 1.0, out_dtype=None, out=None, stream=None):
+    """scale * weight[ids]: rows of weight (num, dim) looked up by int64 or int32 ids of
+    any shape, in out_dtype (weight's type, or any where weight is fp32).  An id outside
+    of the table gives a row of NaN."""
+    wt, num, dim = _table_of(weight)
+    ptr, bits = _ids_of(ids)
+    dtype = _lookup_dtype(weight.dtype, out_dtype)
+    y = _output(out, (*ids.shape, dim), dtype, weight.device, _other(stream), "out")
+    _check(lib().bq_embedding_forward(wt, _dtype_id(dtype, "out"), weight.data_ptr(), num, dim, ptr,
+                                      bits, ids.numel(), scale, y.data_ptr(), _stream(stream)),
+           "bq_embedding_forward")
+    return y
+
+
+def _lookup_grad(dout, ids, dim):
+    import torch
+    ptr, bits = _ids_of(ids)
+    _on_device(dout, "dout")
+    if not dout.is_contiguous() or tuple(dout.shape) != (*ids.shape, dim):
+        raise ValueError(f"dout must be contiguous, of shape {(*ids.shape, dim)}")
+    return ptr, bits, _dtype_id(dout, "dout")
+
+
+def bq_embedding_backward(dout, ids, num: int, padding_idx=None, scale: float = 1.0, dtype=None,
+                          out=None, workspace=None, stream=None):
+    """The gradient of a table of num rows whose rows were looked up by ids: scale times the
+    sums of dout's rows by id, as a dense matrix of dtype (dout's type, or fp32)."""
+    import torch
+    dim = dout.size(-1) if isinstance(dout, torch.Tensor) and dout.dim() else 0
+    ptr, bits, yt = _lookup_grad(dout, ids, dim)
+    dtype = dout.dtype if dtype is None else dtype
+    _lookup_dtype(dtype, dout.dtype)
+    pad = _padding(padding_idx, num)
+    other = _other(stream)
+    dw = _output(out, (num, dim), dtype, dout.device, other, "out")
+    ws = _workspace(workspace, lib().bq_embedding_workspace_bytes(ids.numel(), num, dim),
+                    dout.device, other)
+    _check(lib().bq_embedding_backward(_dtype_id(dtype, "dtype"), yt, dout.data_ptr(), ptr, bits,
+                                       ids.numel(), num, dim, pad, scale, dw.data_ptr(),
+                                       ws.data_ptr(), _stream(stream)), "bq_embedding_backward")
+    return dw
+
+
+def bq_stable_embedding_forward(weight, ids, norm_weight=None, norm_bias=None, eps: float = 1e-5,
+                                out_dtype=None, out=None, stream=None):
+    """The layer norm of weight[ids] (as bq_embedding_forward looks it up) in one pass;
+    norm_weight and norm_bias of weight's type, each may be None."""
+    wt, num, dim = _table_of(weight)
+    ptr, bits = _ids_of(ids)
+    dtype = _lookup_dtype(weight.dtype, out_dtype)
+    w = _vector(norm_weight, dim, weight.dtype, "norm_weight")
+    b = _vector(norm_bias, dim, weight.dtype, "norm_bias")
+    y = _output(out, (*ids.shape, dim), dtype, weight.device, _other(stream), "out")
+    _check(lib().bq_stable_embedding_forward(wt, _dtype_id(dtype, "out"), weight.data_ptr(), num,
+                                             dim, ptr, bits, ids.numel(), w, b, eps, y.data_ptr(),
+                                             _stream(stream)), "bq_stable_embedding_forward")
+    return y
+
+
+def bq_stable_embedding_backward(dout, ids, weight, norm_weight=None, eps: float = 1e-5,
+                                 padding_idx=None, need_norm: bool = True, workspace=None,
+                                 stream=None):
+    """(dweight, dnorm_weight, dnorm_bias) of the stable embedding, in weight's type; the
+    last two None without need_norm."""
+    wt, num, dim = _table_of(weight)
+    ptr, bits, yt = _lookup_grad(dout, ids, dim)
+    _lookup_dtype(weight.dtype, dout.dtype)
+    w = _vector(norm_weight, dim, weight.dtype, "norm_weight")
+    pad = _padding(padding_idx, num)
+    other = _other(stream)
+    dweight = _empty((num, dim), weight.dtype, weight.device, other)
+    dw = db = None
+    if need_norm:
+        dw = _empty((dim,), weight.dtype, weight.device, other)
+        db = _empty((dim,), weight.dtype, weight.device, other)
+    ws = _workspace(workspace, lib().bq_stable_embedding_workspace_bytes(ids.numel(), num, dim),
+                    weight.device, other)
+    _check(lib().bq_stable_embedding_backward(
+        wt, yt, dout.data_ptr(), ptr, bits, ids.numel(), weight.data_ptr(), num, dim, pad, w, eps,
+        dweight.data_ptr(), *(None if t is None else t.data_ptr() for t in (dw, db)),
+        ws.data_ptr(), _stream(stream)), "bq_stable_embedding_backward")
+    return dweight, dw, db
+
+
+def _norm_kind(norm_type):
+    kind = {2.0: BQ_NORM_L2, float("inf"): BQ_NORM_INF}.get(float(norm_type))
+    if kind is None:
+        raise ValueError(f"norm_type must be 2 or inf, got {norm_type}")
+    return kind
+
+
+def _packed(t):
+    """Whether the tensor's elements fill one range of memory, in any order."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for stride, size in sorted(zip(t.stride(), t.shape)):
+        if size > 1:
+            if stride != want:
+                return False
+            want *= size
+    return True
+
+
+def make_grad_array(grads):
+    """Pack gradients (GPU tensors that each fill one range of memory) into a ctypes bq_grad
+    array."""
+    arr = (bq_grad * max(1, len(grads)))()
+    for i, g in enumerate(grads):
+        _on_device(g, f"gradient {i}")
+        if not _packed(g):
+            raise ValueError(f"gradient {i} does not fill one range of memory")
+        arr[i].data = g.data_ptr()
+        arr[i].numel = g.numel()
+        arr[i].dtype = _dtype_id(g, f"gradient {i}")
+    return arr
+
+
+def _grad_norm(grads, norm_type, max_norm, out, workspace, stream):
+    import torch
+    kind = _norm_kind(norm_type)
+    grads = list(grads)
+    arr = make_grad_array(grads)
+    other = _other(stream)
+    device = torch.device("cuda", torch.cuda.current_device())
+    norm = _output(out, (), torch.float32, device, other, "out")
+    ws = _workspace(workspace, lib().bq_grad_norm_workspace_bytes(len(grads)), device, other)
+    if max_norm is None:
+        _check(lib().bq_grad_norm(arr, len(grads), kind, ws.data_ptr(), norm.data_ptr(),
+                                  _stream(stream)), "bq_grad_norm")
+    else:
+        _check(lib().bq_clip_grad_norm(arr, len(grads), kind, max_norm, ws.data_ptr(),
+                                       norm.data_ptr(), _stream(stream)), "bq_clip_grad_norm")
+    return norm
+
+
+def bq_grad_norm(grads, norm_type=2.0, out=None, workspace=None, stream=None):
+    """The norm (2 or inf) of a list of gradients taken as one vector: an fp32 scalar on the
+    GPU."""
+    return _grad_norm(grads, norm_type, None, out, workspace, stream)
+
+
+def bq_clip_grad_norm(grads, max_norm: float, norm_type=2.0, out=None, workspace=None,
+                      stream=None):
+    """The norm as bq_grad_norm; then every gradient times min(1, max_norm / (norm + 1e-6)),
+    in place.  Nothing is read back by the host."""
+    return _grad_norm(grads, norm_type, float(max_norm), out, workspace, stream)

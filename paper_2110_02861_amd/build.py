@@ -23,7 +23,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libbq.so")
 SOURCES = ["bq_api.cpp", "bq_codebook.cpp", "bq_oneshot.hip", "bq_state32.hip",
-           "bq_quantiles.hip"]
+           "bq_quantiles.hip", "bq_ops_api.cpp", "bq_norm.hip", "bq_embedding.hip",
+           "bq_clip.hip"]
 # the benchmark's streaming-ceiling kernel, a library of its own
 STREAM_LIB = os.path.join(PKG, "libbq_stream.so")
 STREAM_SOURCES = ["bq_stream.hip"]
@@ -153,7 +154,7 @@ def build(verbose: bool = False, sanitize: bool = False) -> str:
 def build_asm(out_dir: str) -> None:
     """Write the device assembly of the kernels (for inspection only)."""
     os.makedirs(out_dir, exist_ok=True)
-    for name in ("bq_oneshot.hip", "bq_state32.hip", "bq_quantiles.hip"):
+    for name in (s for s in SOURCES if s.endswith(".hip")):
         cmd = [hipcc(), *FLAGS, "--cuda-device-only", "-S", "-o",
                os.path.join(out_dir, name.replace(".hip", ".s")), os.path.join(CSRC, name)]
         subprocess.run(cmd, check=True)

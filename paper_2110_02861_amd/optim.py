@@ -448,6 +448,13 @@ class Optimizer8bit(torch.optim.Optimizer):
                 if k in s:
                     s[k] = s[k].to(torch.uint8)
 
+    def clip_grad_norm_(self, max_norm: float, norm_type: float = 2.0,
+                        error_if_nonfinite: bool = False) -> torch.Tensor:
+        """Clip the gradients of every param group as one vector (``clip_grad_norm_``), before
+        a step."""
+        return clip_grad_norm_([p for g in self.param_groups for p in g["params"]], max_norm,
+                               norm_type, error_if_nonfinite)
+
     def release_graph_memory(self) -> None:
         """Free every plan pinned by graph capture and everything retired by
         ``load_state_dict``.  Call only once no captured graph that replays
@@ -570,6 +577,46 @@ class Lars8bit(Optimizer8bit):
     def _hparams(self, group, step):
         return dict(lr=group["lr"], beta1=group["momentum"], beta2=0.0, eps=0.0,
                     wd=group["weight_decay"], step=step, trust=group["trust_coefficient"])
+
+
+def _grads_of(parameters):
+    """The gradients of a tensor or an iterable of them, each once."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    seen, grads = set(), []
+    for p in parameters:
+        g = p.grad
+        if g is not None and id(g) not in seen:
+            seen.add(id(g))
+            grads.append(g)
+    return grads
+
+
+def grad_norm(parameters, norm_type: float = 2.0) -> torch.Tensor:
+    """The norm (2 or inf) of the parameters' gradients taken as one vector, as an fp32
+    scalar on the GPU.  Gradients fp32, fp16 or bf16, also mixed, on the current device,
+    each dense in memory; squares are summed in fp64, in one order."""
+    return bq.bq_grad_norm(_grads_of(parameters), norm_type)
+
+
+def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
+                    error_if_nonfinite: bool = False) -> torch.Tensor:
+    """torch.nn.utils.clip_grad_norm_ in HIP kernels: gradients times min(1, max_norm /
+    (norm + 1e-6)) in place; returns the norm from before (``grad_norm``).  Where the norm
+    is within max_norm the gradients are only read.  The host waits for nothing, so the
+    call can be captured into a graph, unless error_if_nonfinite asks for a RuntimeError
+    (with the gradients unchanged) on a norm that is not finite."""
+    if not max_norm >= 0.0:
+        raise ValueError(f"invalid max_norm {max_norm}")
+    grads = _grads_of(parameters)
+    if error_if_nonfinite:
+        norm = bq.bq_grad_norm(grads, norm_type)
+        if not torch.isfinite(norm):
+            raise RuntimeError(f"the gradients' norm is {float(norm)}: they cannot be clipped")
+    norm = bq.bq_clip_grad_norm(grads, max_norm, norm_type)
+    if grads:
+        torch.autograd.graph.increment_version(grads)
+    return norm
 
 
 def _check_hparams(lr, betas, eps, weight_decay):
