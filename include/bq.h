@@ -519,7 +519,7 @@ int64_t bq_embedding_workspace_bytes(int64_t count, int64_t num, int64_t dim);
  *   dout       device, count x dim of out_dtype
  *   dweight    device, num x dim of dtype (every element written)
  *   workspace  device, bq_embedding_workspace_bytes(count, num, dim), 16-byte
- *              aligned (may be NULL where count == 0)
+ *              aligned
  * Errors: as bq_embedding_forward; BQ_ERR_ARG for padding outside [-1, num).
  */
 bq_status bq_embedding_backward(bq_dtype dtype, bq_dtype out_dtype, const void *dout,

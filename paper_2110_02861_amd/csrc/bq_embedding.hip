@@ -4,12 +4,12 @@
 // The gradient of a table's row is the sum of the output gradients of the tokens that
 // looked it up.  The tokens are sorted by id (stable, so a row's tokens stay in their
 // order and the sums have one order), then every row of the table is written once, by
-// the wave that sums its tokens; a row without tokens gets zeros.  Nothing is added
+// whoever sums its tokens; a row without tokens gets zeros.  Nothing is added
 // with floating-point atomics: results are the same bits every time.
 //
-// A row that many tokens share would be one wave's work, so the sorted list is cut into
-// chunks of kChunk positions, and a chunk within one row is summed beforehand by a
-// workgroup of its own; the row's wave then adds that sum in its place.
+// A row that many tokens share would be one workgroup's work, so the sorted list is cut
+// into chunks of kChunk positions, and a chunk within one row is summed beforehand by a
+// workgroup of its own; the row's sum then takes the chunks' sums in their place.
 //
 // The stable embedding's backward pass uses that all tokens of a row look up the same
 // values x, so that xh and rstd are the row's, and the gradient is linear in dy: with S
@@ -65,9 +65,9 @@ __global__ __launch_bounds__(256) void lookup_kernel(const LookupArgs a)
 
 constexpr int kSortThreads = 512;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = 8;                             // per thread and subtile
-constexpr int kSubtile = kSortThreads * kSortItems;       // 4096
-constexpr int kSortTiles = 256;
+constexpr int kSortItems = 2;                             // per thread and subtile
+constexpr int kSubtile = kSortThreads * kSortItems;       // 1024
+constexpr int kSortTiles = 128;
 constexpr int kMaxBins = 1024;
 
 struct SortShape {
@@ -95,7 +95,7 @@ struct SortArgs {
     uint2 *out;
     uint32_t *hist;      // passes x tiles x bins
     int64_t count, num, tile, tiles;
-    int32_t ids64, bits, pass, passes;
+    int32_t ids64, bits, pass, passes, tile_log2;
 };
 
 // Id as a key: ids outside of the table get the key behind its rows.
@@ -126,7 +126,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs
 
 __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs a)
 {
-    __shared__ uint32_t place[kMaxBins];             // next place of each digit
+    __shared__ uint32_t place[kMaxBins];              // next place of each digit
+    __shared__ uint32_t all[kMaxBins];                // of each digit, in all tiles
     __shared__ uint32_t count[kSortWaves][kMaxBins];  // of the subtile, per wave
     __shared__ uint32_t sums[kSortWaves];
     const int n = 1 << a.bits;
@@ -135,20 +136,32 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
     const uint32_t mask = (uint32_t)n - 1;
     const uint32_t *const hist = a.hist + (int64_t)a.pass * a.tiles * n;
 
-    // the digits' counts in all tiles, and in the tiles before this one
+    // the digits' counts in all tiles, and in the tiles before this one: where there
+    // are fewer digits than threads, the threads of a digit share the tiles
+    for (int d = threadIdx.x; d < n; d += kSortThreads)
+        place[d] = all[d] = 0;
+    __syncthreads();
+    const int parts = n < kSortThreads ? kSortThreads >> a.bits : 1;
+    for (int d = threadIdx.x & (n < kSortThreads ? n - 1 : kSortThreads - 1); d < n;
+         d += kSortThreads) {
+        uint32_t total = 0, before = 0;
+#pragma unroll 8
+        for (int t = (int)threadIdx.x >> (n < kSortThreads ? a.bits : 31); t < (int)a.tiles;
+             t += parts) {
+            const uint32_t h = hist[(int64_t)t * n + d];
+            total += h;
+            before += t < (int)blockIdx.x ? h : 0u;
+        }
+        atomicAdd(&all[d], total);
+        atomicAdd(&place[d], before);
+    }
+    __syncthreads();
     const int per = (n + kSortThreads - 1) / kSortThreads;  // 1 or 2 digits per thread
-    uint32_t total[2] = {0, 0}, before[2] = {0, 0};
+    uint32_t mine = 0;
     for (int j = 0; j < per; ++j) {
         const int d = threadIdx.x * per + j;
-        if (d < n) {
-            for (int64_t t = 0; t < a.tiles; ++t) {
-                const uint32_t h = hist[t * n + d];
-                total[j] += h;
-                before[j] += t < (int64_t)blockIdx.x ? h : 0u;
-            }
-        }
+        mine += d < n ? all[d] : 0u;
     }
-    const uint32_t mine = total[0] + total[1];
     const uint32_t incl = wave_scan(mine);
     if (lane == 63)
         sums[wave] = incl;
@@ -158,9 +171,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         run += sums[w];
     for (int j = 0; j < per; ++j) {
         const int d = threadIdx.x * per + j;
-        if (d < n)
-            place[d] = run + before[j];
-        run += total[j];
+        if (d < n) {
+            place[d] += run;
+            run += all[d];
+        }
     }
 
     const int64_t begin = blockIdx.x * a.tile;
@@ -227,7 +241,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
                 const uint32_t at = count[wave][(key[k] >> shift) & mask] + rank[k];
                 a.out[at] = uint2{key[k], pos[k]};
                 if (!last)
-                    atomicAdd(&next[(at / a.tile) * n + ((key[k] >> (shift + a.bits)) & mask)],
+                    atomicAdd(&next[(int64_t)(at >> a.tile_log2) * n + ((key[k] >> (shift + a.bits)) & mask)],
                               1u);
             }
         }
@@ -235,18 +249,22 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
 }
 
 // ---------------------------------------------------------------------------
-// Sums of whole chunks of one row
+// Sums of whole chunks of one row; and where each row of the table starts in the
+// sorted list (a thread per row searches it: all of them wait at the same time).
 // ---------------------------------------------------------------------------
 
-constexpr int kChunk = 64;
+constexpr int kChunk = 32;
+constexpr int kBatch = 8;  // rows in flight per thread
+
+typedef const __attribute__((address_space(4))) uint32_t *cptr;
 
 struct GradArgs {
     LookupGradArgs g;
     const uint2 *sorted;
+    uint32_t *starts;  // num + 1: first position of a key >= i
     float *chunks;     // count / kChunk x dim
     float *partials;   // stable: groups x 2 x dim
-    int64_t groups;
-    int32_t rows_per_team;
+    int32_t chunk_groups;
 };
 
 template <int YT>
@@ -254,8 +272,23 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
 {
     constexpr int V = elem_bytes<YT> == 4 ? 4 : 8;
     __shared__ uint32_t at[kChunk];
+    if ((int)blockIdx.x >= a.chunk_groups) {
+        const int64_t row = (int64_t)(blockIdx.x - a.chunk_groups) * 256 + threadIdx.x;
+        if (row > a.g.num)
+            return;
+        uint32_t lo = 0, hi = (uint32_t)a.g.count;
+        while (lo < hi) {
+            const uint32_t mid = lo + ((hi - lo) >> 1);
+            if ((int64_t)a.sorted[mid].x < row)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        a.starts[row] = lo;
+        return;
+    }
     const int64_t n = a.g.count / kChunk;
-    for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
+    for (int64_t c = blockIdx.x; c < n; c += a.chunk_groups) {
         const uint32_t key = a.sorted[c * kChunk].x;
         // ids outside of the table and the padding row have no gradient; the stable
         // embedding's padding row still has one in the layer norm's parameters
@@ -271,13 +304,16 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
 #pragma unroll
             for (int r = 0; r < V; ++r)
                 s[r] = 0.0f;
-#pragma unroll 8
-            for (int i = 0; i < kChunk; ++i) {
-                float x[V];
-                load_cols<YT, V>(row_of<YT>(a.g.dout, at[i], a.g.dim), col, a.g.dim, x);
+            for (int i = 0; i < kChunk; i += kBatch) {
+                float x[kBatch][V];
 #pragma unroll
-                for (int r = 0; r < V; ++r)
-                    s[r] += x[r];
+                for (int j = 0; j < kBatch; ++j)
+                    load_cols<YT, V>(row_of<YT>(a.g.dout, at[i + j], a.g.dim), col, a.g.dim, x[j]);
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+                    for (int r = 0; r < V; ++r)
+                        s[r] += x[j][r];
             }
             store_cols<kF32, V>(a.chunks + c * a.g.dim, col, a.g.dim, s);
         }
@@ -285,21 +321,82 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// The table's rows.  WAVES waves (a team) hold a row of K vectors of V elements per
-// lane; a plain lookup's longer rows are cut into slabs (blockIdx.y).  A team takes
-// rows_per_team consecutive rows, whose places in the sorted list its lanes search.
+// The table's rows.  A team of lanes holds a row, K vectors of V elements per lane: 16
+// lanes (four teams to a wave), a wave, or a workgroup of as many waves as the row
+// needs; a plain lookup's longer rows are cut into slabs (blockIdx.y).  Teams walk the
+// table with the grid, so that frequent rows, which lie together in many
+// vocabularies, fall to different workgroups.
 // ---------------------------------------------------------------------------
 
-template <int WT, int YT, int WAVES, int K, bool STABLE>
-__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rows_kernel(const GradArgs a)
+enum { kTeam16 = 0, kTeamWave = 1, kTeamGroup = 2 };
+
+// Sum over the team, in every lane; scratch: 16 floats per value.
+template <int TEAM, int N>
+__device__ inline void team_sum(float (&v)[N], float *scratch)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (TEAM == kTeam16) {
+            v[i] = dpp_fadd<0xb1>(v[i]);
+            v[i] = dpp_fadd<0x4e>(v[i]);
+            v[i] = dpp_fadd<0x141>(v[i]);
+            v[i] = dpp_fadd<0x140>(v[i]);
+        } else {
+            v[i] = wave_sum(v[i]);
+        }
+    }
+    if constexpr (TEAM == kTeamGroup) {
+        const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                scratch[i * 16 + wave] = v[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = scratch[i * 16];
+            for (int w = 1; w < waves; ++w)
+                s += scratch[i * 16 + w];
+            v[i] = s;
+        }
+    }
+}
+
+// Adds the columns of N sorted tokens' gradients (of type DT, rows given by `row`).
+template <int DT, int V, int K, int N, typename Row>
+__device__ inline void add_rows(float (&s)[K][V], int64_t c0, int64_t stride, int64_t dim, Row row)
+{
+    float x[N][K][V];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const void *const from = row(j);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            load_cols<DT, V>(from, c0 + k * stride, dim, x[j][k]);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int r = 0; r < V; ++r)
+                s[k][r] += x[j][k][r];
+}
+
+template <int WT, int YT, int TEAM, int K, bool STABLE>
+__global__ __launch_bounds__(TEAM == kTeamGroup ? 1024 : 256) void rows_kernel(const GradArgs a)
 {
     constexpr int V = vec_of<WT, YT>;
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;
-    __shared__ float scratch[5 * WAVES];
-    const int team = WAVES == 1 ? threadIdx.x >> 6 : 0;
-    const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int B = kBatch / K;
+    constexpr int kTeams = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
+    __shared__ float scratch[STABLE && TEAM == kTeamGroup ? 5 * 16 : 1];
+    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
+    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t dim = a.g.dim;
-    const int64_t c0 = (int64_t)blockIdx.y * (64 * WAVES * K * V);
+    const int64_t stride = (int64_t)lanes * V;
+    const int64_t c0 = (int64_t)blockIdx.y * K * stride + lane * V;
     const float rn = 1.0f / (float)dim;
     float dw[K][V], db[K][V];
 #pragma unroll
@@ -308,128 +405,136 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rows_kernel(con
         for (int r = 0; r < V; ++r)
             dw[k][r] = db[k][r] = 0.0f;
 
-    const int rows = a.rows_per_team;
-    const int64_t step = (int64_t)gridDim.x * kTeams * rows;
-    for (int64_t row0 = ((int64_t)blockIdx.x * kTeams + team) * rows; row0 < a.g.num;
-         row0 += step) {
-        // lane i: the first position of a key >= row0 + i (the lanes of every wave alike)
-        const uint32_t want = (uint32_t)(row0 + (threadIdx.x & 63));
-        int64_t lo = 0, hi = a.g.count;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi) >> 1;
-            if (a.sorted[mid].x < want)
-                lo = mid + 1;
-            else
-                hi = mid;
+    // (a workgroup's teams leave together, for the sums over the wave)
+    for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.g.num;
+         row0 += (int64_t)gridDim.x * kTeams) {
+        const int64_t row = row0 + team;
+        const bool exists = row < a.g.num;
+        const bool padding = row == a.g.padding;
+        uint32_t begin = 0, end = 0;
+        if (exists && (STABLE || !padding)) {
+            begin = a.starts[row];
+            end = a.starts[row + 1];
         }
-        for (int i = 0; i < rows && row0 + i < a.g.num; ++i) {
-            const int64_t row = row0 + i;
-            const int64_t begin = __shfl(lo, i), end = __shfl(lo, i + 1);
-            float s[K][V];
+        if constexpr (TEAM != kTeam16) {
+            begin = __builtin_amdgcn_readfirstlane(begin);
+            end = __builtin_amdgcn_readfirstlane(end);
+        }
+        float s[K][V];
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int r = 0; r < V; ++r)
-                    s[k][r] = 0.0f;
-            const bool padding = row == a.g.padding;
-            if (STABLE || !padding) {
-                for (int64_t p = begin; p < end;) {
-                    float x[K][V];
-                    if (p % kChunk == 0 && p + kChunk <= end) {
-                        const float *const from = a.chunks + p / kChunk * dim;
-#pragma unroll
-                        for (int k = 0; k < K; ++k)
-                            load_cols<kF32, V>(from, c0 + (int64_t)(k * 64 * WAVES + lane) * V, dim,
-                                               x[k]);
-                        p += kChunk;
-                    } else {
-                        const void *const from = row_of<YT>(a.g.dout, a.sorted[p].y, dim);
-#pragma unroll
-                        for (int k = 0; k < K; ++k)
-                            load_cols<YT, V>(from, c0 + (int64_t)(k * 64 * WAVES + lane) * V, dim,
-                                             x[k]);
-                        ++p;
-                    }
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-#pragma unroll
-                        for (int r = 0; r < V; ++r)
-                            s[k][r] += x[k][r];
-                }
-            }
-            void *const to = row_of<WT>(a.g.dtable, row, dim);
-            if constexpr (!STABLE) {
+            for (int r = 0; r < V; ++r)
+                s[k][r] = 0.0f;
+        // tokens up to the first whole chunk, the chunks, and the tokens behind them
+        const uint32_t first = (begin + kChunk - 1) / kChunk, last = end / kChunk;
+        const bool chunks = first < last;
+        const auto token = [&](uint32_t p) {
+            // (the sorted list was written by an earlier launch: scalar loads where p is
+            // the same for the wave)
+            const uint32_t at = TEAM == kTeam16 ? a.sorted[p].y : ((cptr)a.sorted)[2 * (uint64_t)p + 1];
+            return row_of<YT>(a.g.dout, at, dim);
+        };
+        const auto tokens = [&](uint32_t p, uint32_t to) {
+            for (; p + B <= to; p += B)
+                add_rows<YT, V, K, B>(s, c0, stride, dim, [&](int j) { return token(p + j); });
+            for (; p < to; ++p)
+                add_rows<YT, V, K, 1>(s, c0, stride, dim, [&](int) { return token(p); });
+        };
+        tokens(begin, chunks ? first * kChunk : end);
+        if (chunks) {
+            uint32_t c = first;
+            const auto chunk = [&](uint32_t i) {
+                return (const void *)(a.chunks + (int64_t)i * dim);
+            };
+            for (; c + B <= last; c += B)
+                add_rows<kF32, V, K, B>(s, c0, stride, dim, [&](int j) { return chunk(c + j); });
+            for (; c < last; ++c)
+                add_rows<kF32, V, K, 1>(s, c0, stride, dim, [&](int) { return chunk(c); });
+            tokens(last * kChunk, end);
+        }
+        void *const to = row_of<WT>(a.g.dtable, exists ? row : 0, dim);
+        if constexpr (!STABLE) {
+            if (exists) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
 #pragma unroll
                     for (int r = 0; r < V; ++r)
                         s[k][r] *= a.g.scale;
-                    store_cols<WT, V>(to, c0 + (int64_t)(k * 64 * WAVES + lane) * V, dim, s[k]);
+                    store_cols<WT, V>(to, c0 + k * stride, dim, s[k]);
                 }
-            } else if (begin == end) {
+            }
+        } else {
+            if (TEAM == kTeam16 ? !__any(begin != end) : begin == end) {
+                if (exists)
 #pragma unroll
-                for (int k = 0; k < K; ++k)
-                    store_cols<WT, V>(to, (int64_t)(k * 64 * WAVES + lane) * V, dim, s[k]);
-            } else {
-                // the row's statistics, as in the forward pass
-                const void *const from = row_of<WT>(a.g.table, row, dim);
-                float x[K][V];
-                float sum[1] = {0.0f};
+                    for (int k = 0; k < K; ++k)
+                        store_cols<WT, V>(to, c0 + k * stride, dim, s[k]);
+                continue;
+            }
+            // the row's statistics, as in the forward pass
+            const void *const from = row_of<WT>(a.g.table, exists ? row : 0, dim);
+            float x[K][V];
+            float sum[1] = {0.0f};
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    load_cols<WT, V>(from, (int64_t)(k * 64 * WAVES + lane) * V, dim, x[k]);
+            for (int k = 0; k < K; ++k) {
+                load_cols<WT, V>(from, c0 + k * stride, dim, x[k]);
 #pragma unroll
-                    for (int r = 0; r < V; ++r)
-                        sum[0] += x[k][r];
+                for (int r = 0; r < V; ++r)
+                    sum[0] += x[k][r];
+            }
+            team_sum<TEAM, 1>(sum, scratch);
+            const float mean0 = sum[0] * rn;
+            float two[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int64_t c = c0 + k * stride;
+#pragma unroll
+                for (int r = 0; r < V; ++r) {
+                    x[k][r] = c + r < dim ? x[k][r] - mean0 : 0.0f;
+                    two[0] += x[k][r];
+                    two[1] = __builtin_fmaf(x[k][r], x[k][r], two[1]);
                 }
-                group_sum<1, WAVES>(sum, scratch);
-                const float mean0 = sum[0] * rn;
-                float two[2] = {0.0f, 0.0f};
+            }
+            team_sum<TEAM, 2>(two, scratch + 16);
+            const float delta = two[0] * rn;
+            float var = two[1] * rn - delta * delta;
+            var = var < 0.0f ? 0.0f : var;
+            const float rstd = 1.0f / sqrtf(var + a.g.eps);
+            const bool some = begin != end;
+            float gs[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
+            for (int k = 0; k < K; ++k) {
+                const int64_t c = c0 + k * stride;
+                float w[V];
 #pragma unroll
-                    for (int r = 0; r < V; ++r) {
-                        x[k][r] = c + r < dim ? x[k][r] - mean0 : 0.0f;
-                        two[0] += x[k][r];
-                        two[1] = __builtin_fmaf(x[k][r], x[k][r], two[1]);
-                    }
-                }
-                group_sum<2, WAVES>(two, scratch + WAVES);
-                const float delta = two[0] * rn;
-                float var = two[1] * rn - delta * delta;
-                var = var < 0.0f ? 0.0f : var;
-                const float rstd = 1.0f / sqrtf(var + a.g.eps);
-                float gs[2] = {0.0f, 0.0f};
+                for (int r = 0; r < V; ++r)
+                    w[r] = 1.0f;
+                if (a.g.weight)
+                    load_cols<WT, V>(a.g.weight, c, dim, w);
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
-                    float w[V];
-#pragma unroll
-                    for (int r = 0; r < V; ++r)
-                        w[r] = 1.0f;
-                    if (a.g.weight)
-                        load_cols<WT, V>(a.g.weight, c, dim, w);
-#pragma unroll
-                    for (int r = 0; r < V; ++r) {
-                        x[k][r] = (x[k][r] - delta) * rstd;
+                for (int r = 0; r < V; ++r) {
+                    x[k][r] = (x[k][r] - delta) * rstd;
+                    if (some)
                         dw[k][r] = __builtin_fmaf(s[k][r], x[k][r], dw[k][r]);
-                        db[k][r] += s[k][r];
-                        s[k][r] *= w[r];
-                        gs[0] += s[k][r];
-                        gs[1] = __builtin_fmaf(s[k][r], x[k][r], gs[1]);
-                    }
+                    db[k][r] += s[k][r];
+                    s[k][r] *= w[r];
+                    gs[0] += s[k][r];
+                    gs[1] = __builtin_fmaf(s[k][r], x[k][r], gs[1]);
                 }
-                group_sum<2, WAVES>(gs, scratch + 3 * WAVES);
-                const float c1 = gs[0] * rn, c2 = gs[1] * rn;
+            }
+            team_sum<TEAM, 2>(gs, scratch + 48);
+            const float c1 = gs[0] * rn, c2 = gs[1] * rn;
+            if (exists) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     float d[V];
 #pragma unroll
                     for (int r = 0; r < V; ++r)
-                        d[r] = padding ? 0.0f
-                                       : rstd * __builtin_fmaf(-x[k][r], c2, s[k][r] - c1);
-                    store_cols<WT, V>(to, (int64_t)(k * 64 * WAVES + lane) * V, dim, d);
+                        d[r] = padding || !some
+                                   ? 0.0f
+                                   : rstd * __builtin_fmaf(-x[k][r], c2, s[k][r] - c1);
+                    store_cols<WT, V>(to, c0 + k * stride, dim, d);
                 }
             }
         }
@@ -437,13 +542,29 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rows_kernel(con
     if constexpr (STABLE) {
         if (!a.partials)
             return;
-        // a partial row for every team
-        float *const out = a.partials + ((int64_t)blockIdx.x * kTeams + team) * 2 * dim;
+        float *const out = a.partials + (int64_t)blockIdx.x * 2 * dim;
+        if constexpr (TEAM == kTeamGroup) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
-            store_cols<kF32, V>(out, c, dim, dw[k]);
-            store_cols<kF32, V>(out + dim, c, dim, db[k]);
+            for (int k = 0; k < K; ++k) {
+                store_cols<kF32, V>(out, c0 + k * stride, dim, dw[k]);
+                store_cols<kF32, V>(out + dim, c0 + k * stride, dim, db[k]);
+            }
+        } else {
+            // the teams' sums, in order (K is 1)
+            __shared__ float join[2][256 * V];
+#pragma unroll
+            for (int r = 0; r < V; ++r) {
+                join[0][threadIdx.x * V + r] = dw[0][r];
+                join[1][threadIdx.x * V + r] = db[0][r];
+            }
+            __syncthreads();
+            for (int64_t c = threadIdx.x; c < 2 * dim; c += 256) {
+                const int which = c >= dim, col = (int)(c - which * dim);
+                float t = join[which][col];
+                for (int i = 1; i < kTeams; ++i)
+                    t += join[which][i * (256 / kTeams) * V + col];
+                out[c] = t;
+            }
         }
     }
 }
@@ -451,9 +572,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void rows_kernel(con
 // Workgroups of the stable embedding's rows: few enough that their partial sums are
 // a small part of the work.
 constexpr int64_t kStableGroups = 512;
+constexpr int64_t kRowGroups = 2048;  // of a plain lookup's rows
 
 struct Layout {
-    int64_t pairs_a, pairs_b, hist, chunks, partials, bytes;
+    int64_t pairs_a, pairs_b, hist, starts, chunks, partials, bytes;
 };
 Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
 {
@@ -462,26 +584,45 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     l.pairs_a = 0;
     l.pairs_b = l.pairs_a + round_up(count * 8, 256);
     l.hist = l.pairs_b + (s.passes > 1 ? round_up(count * 8, 256) : 0);
-    l.chunks = l.hist + round_up((int64_t)s.passes * s.tiles * 4 << s.bits, 256);
+    l.starts = l.hist + round_up((int64_t)s.passes * s.tiles * 4 << s.bits, 256);
+    l.chunks = l.starts + round_up((num + 1) * 4, 256);
     l.partials = l.chunks + round_up(count / kChunk * dim * 4, 256);
-    l.bytes = l.partials + (stable ? kStableGroups * 4 * 2 * dim * 4 : 0);
+    l.bytes = l.partials + (stable ? kStableGroups * 2 * dim * 4 : 0);
     return l;
 }
 
-template <int WT, int YT, int WAVES, int K, bool STABLE>
-void rows_k(GradArgs &a, hipStream_t stream)
+template <int WT, int YT, int TEAM, int K, bool STABLE>
+int64_t rows_k(const GradArgs &a, int threads, hipStream_t stream)
 {
     constexpr int V = vec_of<WT, YT>;
-    constexpr int kTeams = WAVES == 1 ? 4 : 1;
-    const int64_t slab = 64 * WAVES * K * V;
-    const int64_t teams = (a.g.num + a.rows_per_team - 1) / a.rows_per_team;
-    int64_t groups = (teams + kTeams - 1) / kTeams;
-    const int64_t most = STABLE ? kStableGroups : int64_t{1} << 20;
+    constexpr int kTeams = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
+    const int64_t slab = (int64_t)threads / kTeams * K * V;
+    const int64_t most = STABLE ? kStableGroups : kRowGroups;
+    int64_t groups = (a.g.num + kTeams - 1) / kTeams;
     groups = groups < most ? groups : most;
-    a.groups = groups * kTeams;
-    hipLaunchKernelGGL((rows_kernel<WT, YT, WAVES, K, STABLE>),
-                       dim3((unsigned)groups, STABLE ? 1u : (unsigned)((a.g.dim + slab - 1) / slab)),
-                       dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, stream, a);
+    hipLaunchKernelGGL((rows_kernel<WT, YT, TEAM, K, STABLE>),
+                       dim3((unsigned)groups, (unsigned)((a.g.dim + slab - 1) / slab)),
+                       dim3((unsigned)threads), 0, stream, a);
+    return groups;
+}
+
+// The team that holds a row, and the launch; returns the workgroups.
+template <int WT, int YT, bool STABLE>
+int64_t rows(const GradArgs &a, hipStream_t stream)
+{
+    constexpr int V = vec_of<WT, YT>;
+    const int64_t vectors = (a.g.dim + V - 1) / V;
+    if (vectors <= 16)
+        return rows_k<WT, YT, kTeam16, 1, STABLE>(a, 256, stream);
+    if (vectors <= 64)
+        return rows_k<WT, YT, kTeamWave, 1, STABLE>(a, 256, stream);
+    if (vectors <= 1024)
+        return rows_k<WT, YT, kTeamGroup, 1, STABLE>(a, (int)((vectors + 63) / 64 * 64), stream);
+    if constexpr (STABLE && V == 4) {
+        if (vectors > 2048)
+            return rows_k<WT, YT, kTeamGroup, 4, STABLE>(a, 1024, stream);
+    }
+    return rows_k<WT, YT, kTeamGroup, 2, STABLE>(a, 1024, stream);
 }
 
 template <int WT, int YT>
@@ -493,12 +634,10 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
     GradArgs a;
     a.g = g;
     a.sorted = nullptr;
+    a.starts = reinterpret_cast<uint32_t *>(g.workspace + l.starts);
     a.chunks = reinterpret_cast<float *>(g.workspace + l.chunks);
     a.partials = stable && (g.dweight || g.dbias)
                      ? reinterpret_cast<float *>(g.workspace + l.partials) : nullptr;
-    a.groups = 0;
-    // consecutive rows share a search; small tables need every wave
-    a.rows_per_team = g.num >= 65536 ? 8 : g.num >= 16384 ? 4 : 1;
 
     if (g.count > 0) {
         uint2 *const pa = reinterpret_cast<uint2 *>(g.workspace + l.pairs_a);
@@ -514,6 +653,7 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
         s.tiles = shape.tiles;
         s.ids64 = g.ids64;
         s.bits = shape.bits;
+        s.tile_log2 = 63 - __builtin_clzll((unsigned long long)shape.tile);
         s.passes = shape.passes;
         s.pass = 0;
         const dim3 grid((unsigned)shape.tiles), block(kSortThreads);
@@ -524,43 +664,22 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
             s.in = s.out;
         }
         a.sorted = s.in;
-        const int64_t chunks = g.count / kChunk;
-        if (chunks > 0)
-            hipLaunchKernelGGL(chunk_kernel<YT>, dim3((unsigned)(chunks < 65536 ? chunks : 65536)),
-                               dim3(256), 0, stream, a);
     }
+    const int64_t chunks = g.count / kChunk;
+    a.chunk_groups = (int32_t)(chunks < 65536 ? chunks : 65536);
+    hipLaunchKernelGGL(chunk_kernel<YT>,
+                       dim3((unsigned)(a.chunk_groups + (g.num + 1 + 255) / 256)), dim3(256), 0,
+                       stream, a);
 
-    constexpr int kMost = 32 / vec_of<WT, YT>;  // vectors per lane
-    const int64_t k = (g.dim + 64 * vec_of<WT, YT> - 1) / (64 * vec_of<WT, YT>);
     if (!stable) {
-        if (k <= 1)
-            rows_k<WT, YT, 1, 1, false>(a, stream);
-        else if (k <= 2)
-            rows_k<WT, YT, 1, 2, false>(a, stream);
-        else if (k <= 4)
-            rows_k<WT, YT, 1, 4, false>(a, stream);
-        else
-            rows_k<WT, YT, 1, kMost, false>(a, stream);
+        rows<WT, YT, false>(a, stream);
         return hipGetLastError();
     }
-    if (k <= 1)
-        rows_k<WT, YT, 1, 1, true>(a, stream);
-    else if (k <= 2)
-        rows_k<WT, YT, 1, 2, true>(a, stream);
-    else if (k <= 4)
-        rows_k<WT, YT, 1, 4, true>(a, stream);
-    else if (k <= kMost)
-        rows_k<WT, YT, 1, kMost, true>(a, stream);
-    else if (k <= 2 * kMost)
-        rows_k<WT, YT, 4, kMost / 2, true>(a, stream);
-    else if (k <= 4 * kMost)
-        rows_k<WT, YT, 4, kMost, true>(a, stream);
-    else
-        rows_k<WT, YT, 16, kMost / 2, true>(a, stream);
+    const int64_t groups = rows<WT, YT, true>(a, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.partials)
         return e;
-    return launch_param_grads(WT, a.partials, a.groups, g.dim, g.dweight, g.dbias, stream);
+    return launch_param_grads(WT, a.partials, groups, g.dim, g.dweight, g.dbias, stream);
 }
 
 }  // namespace

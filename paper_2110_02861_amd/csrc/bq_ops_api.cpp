@@ -185,7 +185,7 @@ bq_status bq_embedding_backward(bq_dtype dtype, bq_dtype out_dtype, const void *
         return st;
     if (!std::isfinite(scale) || padding < -1 || padding >= num)
         return BQ_ERR_ARG;
-    if (!dweight || (count > 0 && (!dout || !ids || !workspace)))
+    if (!dweight || !workspace || (count > 0 && (!dout || !ids)))
         return BQ_ERR_NULL;
     if (!elements(dout, out_dtype) || !elements(dweight, dtype) || !aligned(ids, id_bits / 8) ||
         !aligned(workspace, 16))

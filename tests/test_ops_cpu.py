@@ -80,7 +80,8 @@ EMBB = dict(dtype=F, out=F, dy=A, ids=A, bits=64, count=4, num=100, dim=8, paddi
     (dict(dtype=H, out=F), DTYPE), (dict(bits=8), DTYPE), (dict(num=0), SIZE),
     (dict(count=1 << 31), SIZE), (dict(padding=-2), ARG), (dict(padding=100), ARG),
     (dict(scale=NAN), ARG), (dict(dy=None), NULL), (dict(ids=None), NULL), (dict(dw=None), NULL),
-    (dict(ws=None), NULL), (dict(ws=A + 8), ALIGN), (dict(dy=ODD), ALIGN), (dict(dw=ODD), ALIGN)])
+    (dict(ws=None), NULL), (dict(count=0, ws=None), NULL), (dict(ws=A + 8), ALIGN),
+    (dict(dy=ODD), ALIGN), (dict(dw=ODD), ALIGN)])
 def test_embedding_backward(change, want):
     assert call("bq_embedding_backward", EMBB, **change) == want
 
