@@ -154,13 +154,18 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
-# csrc/bq_host.cpp: the ordinary case of the calls below in native code.  Each of
+# csrc/bq_host*.cpp: the ordinary case of the calls below in native code.  Each of
 # its functions returns None where the Python code after it is to run (errors,
 # tensors of other classes, active torch modes).
 _HOST_CALLS = ("bq_quantize_blockwise", "bq_quantize_blockwise_prepared",
                "bq_dequantize_blockwise", "bq_estimate_quantile_codebook",
                "bq_quantile_workspace_bytes", "bq_optimizer8bit_step", "bq_step_plan_run",
                "bq_step_plan_run_prepared")
+_HOST_OPS = ("bq_layer_norm_forward", "bq_layer_norm_workspace_bytes", "bq_layer_norm_backward",
+             "bq_embedding_forward", "bq_embedding_workspace_bytes", "bq_embedding_backward",
+             "bq_stable_embedding_forward", "bq_stable_embedding_workspace_bytes",
+             "bq_stable_embedding_backward", "bq_grad_norm_workspace_bytes", "bq_grad_norm",
+             "bq_clip_grad_norm")
 _host_module = None
 
 
@@ -180,8 +185,8 @@ def host():
         import torch  # noqa: F401  (the module links against it)
         try:
             from . import _bqhost
-            _bqhost.bind(tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value
-                               for n in _HOST_CALLS))
+            for bind, names in ((_bqhost.bind, _HOST_CALLS), (_bqhost.bind_ops, _HOST_OPS)):
+                bind(tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
             _host_module = _bqhost
         except ImportError as e:
             _host_module = _PythonOnly()
@@ -746,6 +751,10 @@ def bq_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, stats: b
     """The layer norm of x over its last dimension; with stats, (y, mean, rstd), the
     fp32 statistics of every row that the backward pass takes.  weight and bias: of
     x's type or fp32, both alike, each may be None."""
+    if not stats and out is None and stream is None:
+        y = host().layer_norm(x, weight, bias, eps, False)
+        if y is not None:
+            return y
     import torch
     rows, cols, stride = _rows_of(x, "x")
     xt = _dtype_id(x, "x")
@@ -840,6 +849,10 @@ def bq_embedding_forward(weight, ids, scale: float = 1.0, out_dtype=None, out=No
     """scale * weight[ids]: rows of weight (num, dim) looked up by int64 or int32 ids of
     any shape, in out_dtype (weight's type, or any where weight is fp32).  An id outside
     of the table gives a row of NaN."""
+    if out is None and stream is None:
+        y = host().embedding(ids, weight, None, scale, out_dtype, False)
+        if y is not None:
+            return y
     wt, num, dim = _table_of(weight)
     ptr, bits = _ids_of(ids)
     dtype = _lookup_dtype(weight.dtype, out_dtype)
@@ -883,6 +896,11 @@ def bq_stable_embedding_forward(weight, ids, norm_weight=None, norm_bias=None, e
                                 out_dtype=None, out=None, stream=None):
     """The layer norm of weight[ids] (as bq_embedding_forward looks it up) in one pass;
     norm_weight and norm_bias of weight's type, each may be None."""
+    if out is None and stream is None:
+        y = host().stable_embedding(ids, weight, norm_weight, norm_bias, eps, None, out_dtype,
+                                    False)
+        if y is not None:
+            return y
     wt, num, dim = _table_of(weight)
     ptr, bits = _ids_of(ids)
     dtype = _lookup_dtype(weight.dtype, out_dtype)

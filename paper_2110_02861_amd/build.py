@@ -32,7 +32,7 @@ ARCH = "gfx950"
 
 # the native half of the Python binding (module _bqhost), built against torch
 HOST_LIB = os.path.join(PKG, "_bqhost.so")
-HOST_SOURCE = "bq_host.cpp"
+HOST_SOURCES = ["bq_host.cpp", "bq_host_ops.cpp"]
 
 # -ffp-contract=off: the state arithmetic must not be fused into fma, so that it
 # rounds exactly as its definition.  Packed fp32 instructions are disabled.
@@ -118,7 +118,8 @@ def host_command(out: str) -> list:
             "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
             "-isystem", os.path.join(rocm, "include"),
             "-isystem", sysconfig.get_paths()["include"],
-            "-I", os.path.join(ROOT, "include"), "-o", out, os.path.join(CSRC, HOST_SOURCE),
+            "-I", os.path.join(ROOT, "include"), "-o", out,
+            *(os.path.join(CSRC, s) for s in HOST_SOURCES),
             "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
 
 

@@ -13,10 +13,7 @@
 // dequantize of 300,007 values 21.8 and 8.1 us; replayed steps of the drop-in momentum
 // on the ResNet-50 list (161 tensors) 90.4 and 57.5 us, which is the kernel's time, and
 // of the drop-in Adam on 6 small tensors 21.2 and 13.6 us.
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include <initializer_list>
+#include "bq_host.h"
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
@@ -31,6 +28,8 @@
 
 namespace {
 
+using namespace bq_host;
+
 // Entry points of the libbq.so that bq.py loaded (addresses passed to bind).
 struct Library {
     decltype(&bq_quantize_blockwise) quantize;
@@ -43,21 +42,6 @@ struct Library {
     decltype(&bq_step_plan_run_prepared) run_prepared;
 } lib;
 
-// Thrown where the Python code is to run instead (errors and unusual
-// arguments included).
-struct NotHandled {};
-
-void need(bool ok)
-{
-    if (!ok)
-        throw NotHandled{};
-}
-
-PyObject *none()
-{
-    Py_RETURN_NONE;
-}
-
 // Calls that are left to Python as a matter of course, found without a throw
 // (which takes 2 us).
 //
@@ -67,15 +51,6 @@ bool modes()
 {
     return c10::impl::TorchDispatchModeTLS::any_modes_set() ||
            at::impl::PythonTorchFunctionTLS::stack_len() != 0;
-}
-
-// Whether every argument is None or of exactly torch's own classes.
-bool plain(std::initializer_list<PyObject *> tensors)
-{
-    for (PyObject *o : tensors)
-        if (o != Py_None && !THPVariable_CheckExact(o))
-            return false;
-    return true;
 }
 
 // A contiguous tensor of exactly torch's own classes on the current device.
@@ -103,17 +78,6 @@ void *buffer(PyObject *o, int64_t bytes, int device)
     need(t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device &&
          t.is_contiguous() && t.numel() * static_cast<int64_t>(t.element_size()) >= bytes);
     return t.data_ptr();
-}
-
-// An int, or any other object that stands for one (numpy's).
-int64_t whole(PyObject *o)
-{
-    const long long v = PyLong_AsLongLong(o);  // by __index__
-    if (v == -1 && PyErr_Occurred()) {
-        PyErr_Clear();
-        throw NotHandled{};
-    }
-    return v;
 }
 
 int32_t whole32(PyObject *o)
@@ -172,21 +136,6 @@ bq_hparams hparams(PyObject *dict)
     h.step = whole(step);
     h.trust_coeff = number(dict, "trust", false, 0.0f);
     return h;
-}
-
-// Runs f, which returns a new reference, and hands anything unusual to Python.
-template <class F>
-PyObject *handled(F f)
-{
-    try {
-        return f();
-    } catch (const NotHandled &) {
-    } catch (const std::exception &) {
-        // e.g. a tensor without storage: the Python code meets it again and
-        // raises its error
-    }
-    PyErr_Clear();
-    return none();
 }
 
 // The C call without the interpreter lock, as ctypes makes it (a launch waits
@@ -522,4 +471,12 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bqhost", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__bqhost() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__bqhost()
+{
+    PyObject *const m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, bq_ops_methods) != 0) {
+        Py_DECREF(m);
+        return nullptr;
+    }
+    return m;
+}

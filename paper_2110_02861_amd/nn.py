@@ -69,6 +69,9 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     """The layer norm of x over its last dimension: (x - mean) / sqrt(var + eps) * weight +
     bias.  x in fp32, fp16 or bf16; weight and bias of that type or fp32, each may be
     None.  Statistics and sums are fp32."""
+    y = bq.host().layer_norm(x, weight, bias, eps, True)
+    if y is not None:
+        return y
     with _device_of(x, "x"):
         x = _packed_rows(x)
         if _wants_grad(x, weight, bias):
@@ -99,6 +102,9 @@ def embedding(ids, weight, padding_idx=None, scale: float = 1.0, out_dtype=None)
     that is summed by sorted ids, in fp32 and in one order.  ids: int64 or int32, any
     shape; out_dtype: weight's type, or any of the three where weight is fp32.  An id
     outside of the table gives a row of NaN and no gradient."""
+    y = bq.host().embedding(ids, weight, padding_idx, scale, out_dtype, True)
+    if y is not None:
+        return y
     with _device_of(weight, "weight"):
         bq._padding(padding_idx, weight.size(0))
         ids = ids.contiguous()
@@ -136,6 +142,10 @@ def stable_embedding(ids, weight, norm_weight=None, norm_bias=None, eps: float =
     rows are never in memory, and the backward pass takes the layer norm's gradient once
     per distinct id.  All parameters have weight's type; rows of up to
     bq.BQ_STABLE_EMBEDDING_MAX_DIM elements.  The other arguments as ``embedding``."""
+    y = bq.host().stable_embedding(ids, weight, norm_weight, norm_bias, eps, padding_idx,
+                                   out_dtype, True)
+    if y is not None:
+        return y
     with _device_of(weight, "weight"):
         bq._padding(padding_idx, weight.size(0))
         ids = ids.contiguous()

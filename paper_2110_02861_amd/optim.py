@@ -579,10 +579,12 @@ class Lars8bit(Optimizer8bit):
                     wd=group["weight_decay"], step=step, trust=group["trust_coefficient"])
 
 
+def _list_of(parameters):
+    return [parameters] if isinstance(parameters, torch.Tensor) else list(parameters)
+
+
 def _grads_of(parameters):
-    """The gradients of a tensor or an iterable of them, each once."""
-    if isinstance(parameters, torch.Tensor):
-        parameters = [parameters]
+    """The gradients of a list of tensors, each once."""
     seen, grads = set(), []
     for p in parameters:
         g = p.grad
@@ -596,7 +598,9 @@ def grad_norm(parameters, norm_type: float = 2.0) -> torch.Tensor:
     """The norm (2 or inf) of the parameters' gradients taken as one vector, as an fp32
     scalar on the GPU.  Gradients fp32, fp16 or bf16, also mixed, on the current device,
     each dense in memory; squares are summed in fp64, in one order."""
-    return bq.bq_grad_norm(_grads_of(parameters), norm_type)
+    parameters = _list_of(parameters)
+    norm = bq.host().clip(parameters, None, bq._norm_kind(norm_type))
+    return bq.bq_grad_norm(_grads_of(parameters), norm_type) if norm is None else norm
 
 
 def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
@@ -608,11 +612,15 @@ def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
     (with the gradients unchanged) on a norm that is not finite."""
     if not max_norm >= 0.0:
         raise ValueError(f"invalid max_norm {max_norm}")
-    grads = _grads_of(parameters)
+    parameters = _list_of(parameters)
     if error_if_nonfinite:
-        norm = bq.bq_grad_norm(grads, norm_type)
+        norm = grad_norm(parameters, norm_type)
         if not torch.isfinite(norm):
             raise RuntimeError(f"the gradients' norm is {float(norm)}: they cannot be clipped")
+    norm = bq.host().clip(parameters, max_norm, bq._norm_kind(norm_type))
+    if norm is not None:
+        return norm
+    grads = _grads_of(parameters)
     norm = bq.bq_clip_grad_norm(grads, max_norm, norm_type)
     if grads:
         torch.autograd.graph.increment_version(grads)
