@@ -501,7 +501,7 @@ bq_status bq_layer_norm_backward(bq_dtype dtype, bq_dtype param_dtype, const voi
  *            [0, num) reads nothing and gives a row of NaN
  *   out      device, count x dim (written)
  * Errors: BQ_ERR_DTYPE (types, id_bits), BQ_ERR_SIZE (count < 0 or >= 2^31,
- * num < 1 or >= 2^31 - 1, dim < 1 or > 2^30), BQ_ERR_ARG (scale not finite),
+ * num < 1 or >= 2^31 - 1, dim < 1 or > 2^24), BQ_ERR_ARG (scale not finite),
  * BQ_ERR_NULL, BQ_ERR_ALIGN, BQ_ERR_HIP.
  */
 bq_status bq_embedding_forward(bq_dtype dtype, bq_dtype out_dtype, const void *weight, int64_t num,

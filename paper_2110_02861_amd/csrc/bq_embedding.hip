@@ -31,27 +31,45 @@ constexpr int vec_of = (elem_bytes<A> == 4 || elem_bytes<B> == 4) ? 4 : 8;
 constexpr float kNaN = __builtin_nanf("");
 
 // ---------------------------------------------------------------------------
-// Lookup: a wave per token.
+// Lookup.  A team takes four tokens at a time, whose rows' loads are in flight together;
+// longer rows are cut into slabs (blockIdx.y).
 // ---------------------------------------------------------------------------
 
-template <int WT, int YT>
-__global__ __launch_bounds__(256) void lookup_kernel(const LookupArgs a)
+constexpr int kLookups = 4;
+
+template <int WT, int YT, int TEAM, bool TAIL>
+__global__ __launch_bounds__(most_threads<TEAM>) void lookup_kernel(const LookupArgs a)
 {
     constexpr int V = vec_of<WT, YT>;
-    const int lane = threadIdx.x & 63;
-    for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < a.count;
-         t += (int64_t)gridDim.x * 4) {
-        const int64_t id = id_at(a.ids, t, a.ids64);
-        const bool known = id >= 0 && id < a.num;
-        const void *const from = row_of<WT>(a.table, known ? id : 0, a.dim);
-        void *const to = row_of<YT>(a.out, t, a.dim);
-        for (int64_t c = lane * V; c < a.dim; c += 64 * V) {
-            float x[V];
-            load_cols<WT, V>(from, c, a.dim, x);
+    constexpr int kTeams = teams_of<TEAM>;
+    using C = Cols<V, 1, TAIL>;
+    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
+    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
+    const C c(a.dim, lane, lanes, (int64_t)blockIdx.y * lanes * V);
+    for (int64_t t0 = ((int64_t)blockIdx.x * kTeams + team) * kLookups; t0 < a.count;
+         t0 += (int64_t)gridDim.x * kTeams * kLookups) {
+        int64_t id[kLookups];
+        RawRow<WT, V, 1, TAIL> raw[kLookups];
 #pragma unroll
-            for (int r = 0; r < V; ++r)
-                x[r] = known ? x[r] * a.scale : kNaN;
-            store_cols<YT, V>(to, c, a.dim, x);
+        for (int j = 0; j < kLookups; ++j)
+            id[j] = id_at(a.ids, t0 + j < a.count ? t0 + j : a.count - 1, a.ids64);
+#pragma unroll
+        for (int j = 0; j < kLookups; ++j) {
+            const bool known = id[j] >= 0 && id[j] < a.num;
+            load_row<WT, false>(c, row_of<WT>(a.table, known ? id[j] : 0, a.dim), raw[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kLookups; ++j) {
+            if (t0 + j >= a.count)
+                break;
+            const bool known = id[j] >= 0 && id[j] < a.num;
+            float x[C::kElems];
+            unpack<WT, V, 1, TAIL>(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < C::kElems; ++e)
+                x[e] = known ? x[e] * a.scale : kNaN;
+            store_row<YT>(c, row_of<YT>(a.out, t0 + j, a.dim), x);
         }
     }
 }
@@ -299,111 +317,84 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
         if (threadIdx.x < kChunk)
             at[threadIdx.x] = a.sorted[c * kChunk + threadIdx.x].y;
         __syncthreads();
-        for (int64_t col = (int64_t)threadIdx.x * V; col < a.g.dim; col += 256 * V) {
+        float *const out = a.chunks + c * a.g.dim;
+        const int64_t whole = a.g.dim / V * V;
+        for (int64_t col = (int64_t)threadIdx.x * V; col < whole; col += 256 * V) {
             float s[V];
 #pragma unroll
             for (int r = 0; r < V; ++r)
                 s[r] = 0.0f;
             for (int i = 0; i < kChunk; i += kBatch) {
-                float x[kBatch][V];
+                Raw<YT, V> x[kBatch];
 #pragma unroll
                 for (int j = 0; j < kBatch; ++j)
-                    load_cols<YT, V>(row_of<YT>(a.g.dout, at[i + j], a.g.dim), col, a.g.dim, x[j]);
+                    x[j] = load_raw<YT, V, false>(row_of<YT>(a.g.dout, at[i + j], a.g.dim), col);
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j)
+                for (int j = 0; j < kBatch; ++j) {
+                    float f[V];
+                    unpack<YT, V>(x[j], f);
 #pragma unroll
                     for (int r = 0; r < V; ++r)
-                        s[r] += x[j][r];
+                        s[r] += f[r];
+                }
             }
-            store_cols<kF32, V>(a.chunks + c * a.g.dim, col, a.g.dim, s);
+            store_vec<kF32, V>(out, col, s);
+        }
+        const int64_t col = whole + threadIdx.x;
+        if (col < a.g.dim) {
+            float s = 0.0f;
+            for (int i = 0; i < kChunk; ++i)
+                s += load1<YT>(row_of<YT>(a.g.dout, at[i], a.g.dim), col);
+            out[col] = s;
         }
     }
 }
 
 // ---------------------------------------------------------------------------
-// The table's rows.  A team of lanes holds a row, K vectors of V elements per lane: 16
-// lanes (four teams to a wave), a wave, or a workgroup of as many waves as the row
-// needs; a plain lookup's longer rows are cut into slabs (blockIdx.y).  Teams walk the
+// The table's rows.  A team of lanes holds a row, K vectors of V elements per lane; a
+// plain lookup's longer rows are cut into slabs (blockIdx.y).  Teams walk the
 // table with the grid, so that frequent rows, which lie together in many
 // vocabularies, fall to different workgroups.
 // ---------------------------------------------------------------------------
 
-enum { kTeam16 = 0, kTeamWave = 1, kTeamGroup = 2 };
-
-// Sum over the team, in every lane; scratch: 16 floats per value.
-template <int TEAM, int N>
-__device__ inline void team_sum(float (&v)[N], float *scratch)
+// Adds N rows of type DT, given by `row`, to a lane's columns.
+template <int DT, int N, int V, int K, bool TAIL, typename Row>
+__device__ inline void add_rows(const Cols<V, K, TAIL> &c, float (&s)[Cols<V, K, TAIL>::kElems],
+                                Row row)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if constexpr (TEAM == kTeam16) {
-            v[i] = dpp_fadd<0xb1>(v[i]);
-            v[i] = dpp_fadd<0x4e>(v[i]);
-            v[i] = dpp_fadd<0x141>(v[i]);
-            v[i] = dpp_fadd<0x140>(v[i]);
-        } else {
-            v[i] = wave_sum(v[i]);
-        }
-    }
-    if constexpr (TEAM == kTeamGroup) {
-        const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-        if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                scratch[i * 16 + wave] = v[i];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            float s = scratch[i * 16];
-            for (int w = 1; w < waves; ++w)
-                s += scratch[i * 16 + w];
-            v[i] = s;
-        }
-    }
-}
-
-// Adds the columns of N sorted tokens' gradients (of type DT, rows given by `row`).
-template <int DT, int V, int K, int N, typename Row>
-__device__ inline void add_rows(float (&s)[K][V], int64_t c0, int64_t stride, int64_t dim, Row row)
-{
-    float x[N][K][V];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-        const void *const from = row(j);
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-            load_cols<DT, V>(from, c0 + k * stride, dim, x[j][k]);
-    }
+    RawRow<DT, V, K, TAIL> x[N];
 #pragma unroll
     for (int j = 0; j < N; ++j)
+        load_row<DT, false>(c, row(j), x[j]);
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+    for (int j = 0; j < N; ++j) {
+        float f[Cols<V, K, TAIL>::kElems];
+        unpack<DT, V, K, TAIL>(x[j], f);
 #pragma unroll
-            for (int r = 0; r < V; ++r)
-                s[k][r] += x[j][k][r];
+        for (int e = 0; e < Cols<V, K, TAIL>::kElems; ++e)
+            s[e] += f[e];
+    }
 }
 
-template <int WT, int YT, int TEAM, int K, bool STABLE>
-__global__ __launch_bounds__(TEAM == kTeamGroup ? 1024 : 256) void rows_kernel(const GradArgs a)
+template <int WT, int YT, int TEAM, int K, bool STABLE, bool TAIL>
+__global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs a)
 {
     constexpr int V = vec_of<WT, YT>;
     constexpr int B = kBatch / K;
-    constexpr int kTeams = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
+    constexpr int kTeams = teams_of<TEAM>;
+    using C = Cols<V, K, TAIL>;
+    constexpr int E = C::kElems;
     __shared__ float scratch[STABLE && TEAM == kTeamGroup ? 5 * 16 : 1];
     const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
     const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
     const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t dim = a.g.dim;
-    const int64_t stride = (int64_t)lanes * V;
-    const int64_t c0 = (int64_t)blockIdx.y * K * stride + lane * V;
+    const C c(dim, lane, lanes, (int64_t)blockIdx.y * lanes * K * V);
     const float rn = 1.0f / (float)dim;
-    float dw[K][V], db[K][V];
+    float dw[E], db[E];
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int r = 0; r < V; ++r)
-            dw[k][r] = db[k][r] = 0.0f;
+    for (int e = 0; e < E; ++e)
+        dw[e] = db[e] = 0.0f;
 
     // (a workgroup's teams leave together, for the sums over the wave)
     for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.g.num;
@@ -420,152 +411,102 @@ __global__ __launch_bounds__(TEAM == kTeamGroup ? 1024 : 256) void rows_kernel(c
             begin = __builtin_amdgcn_readfirstlane(begin);
             end = __builtin_amdgcn_readfirstlane(end);
         }
-        float s[K][V];
+        float s[E];
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int r = 0; r < V; ++r)
-                s[k][r] = 0.0f;
+        for (int e = 0; e < E; ++e)
+            s[e] = 0.0f;
         // tokens up to the first whole chunk, the chunks, and the tokens behind them
         const uint32_t first = (begin + kChunk - 1) / kChunk, last = end / kChunk;
         const bool chunks = first < last;
         const auto token = [&](uint32_t p) {
             // (the sorted list was written by an earlier launch: scalar loads where p is
             // the same for the wave)
-            const uint32_t at = TEAM == kTeam16 ? a.sorted[p].y : ((cptr)a.sorted)[2 * (uint64_t)p + 1];
+            const uint32_t at = TEAM == kTeam16 ? a.sorted[p].y
+                                                : ((cptr)a.sorted)[2 * (uint64_t)p + 1];
             return row_of<YT>(a.g.dout, at, dim);
         };
         const auto tokens = [&](uint32_t p, uint32_t to) {
             for (; p + B <= to; p += B)
-                add_rows<YT, V, K, B>(s, c0, stride, dim, [&](int j) { return token(p + j); });
+                add_rows<YT, B>(c, s, [&](int j) { return token(p + j); });
             for (; p < to; ++p)
-                add_rows<YT, V, K, 1>(s, c0, stride, dim, [&](int) { return token(p); });
+                add_rows<YT, 1>(c, s, [&](int) { return token(p); });
         };
         tokens(begin, chunks ? first * kChunk : end);
         if (chunks) {
-            uint32_t c = first;
-            const auto chunk = [&](uint32_t i) {
-                return (const void *)(a.chunks + (int64_t)i * dim);
+            uint32_t i = first;
+            const auto chunk = [&](uint32_t k) {
+                return (const void *)(a.chunks + (int64_t)k * dim);
             };
-            for (; c + B <= last; c += B)
-                add_rows<kF32, V, K, B>(s, c0, stride, dim, [&](int j) { return chunk(c + j); });
-            for (; c < last; ++c)
-                add_rows<kF32, V, K, 1>(s, c0, stride, dim, [&](int) { return chunk(c); });
+            for (; i + B <= last; i += B)
+                add_rows<kF32, B>(c, s, [&](int j) { return chunk(i + j); });
+            for (; i < last; ++i)
+                add_rows<kF32, 1>(c, s, [&](int) { return chunk(i); });
             tokens(last * kChunk, end);
         }
         void *const to = row_of<WT>(a.g.dtable, exists ? row : 0, dim);
         if constexpr (!STABLE) {
-            if (exists) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-#pragma unroll
-                    for (int r = 0; r < V; ++r)
-                        s[k][r] *= a.g.scale;
-                    store_cols<WT, V>(to, c0 + k * stride, dim, s[k]);
-                }
-            }
+            for (int e = 0; e < E; ++e)
+                s[e] *= a.g.scale;
+            if (exists)
+                store_row<WT>(c, to, s);
         } else {
-            if (TEAM == kTeam16 ? !__any(begin != end) : begin == end) {
+            const bool some = begin != end;
+            if (TEAM == kTeam16 ? !__any(some) : !some) {
                 if (exists)
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-                        store_cols<WT, V>(to, c0 + k * stride, dim, s[k]);
+                    store_row<WT>(c, to, s);
                 continue;
             }
             // the row's statistics, as in the forward pass
-            const void *const from = row_of<WT>(a.g.table, exists ? row : 0, dim);
-            float x[K][V];
+            float x[E];
             float sum[1] = {0.0f};
+            load_floats<WT, V, K, TAIL>(c, row_of<WT>(a.g.table, exists ? row : 0, dim), x);
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                load_cols<WT, V>(from, c0 + k * stride, dim, x[k]);
-#pragma unroll
-                for (int r = 0; r < V; ++r)
-                    sum[0] += x[k][r];
-            }
+            for (int e = 0; e < E; ++e)
+                sum[0] += x[e];
             team_sum<TEAM, 1>(sum, scratch);
             const float mean0 = sum[0] * rn;
             float two[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int64_t c = c0 + k * stride;
-#pragma unroll
-                for (int r = 0; r < V; ++r) {
-                    x[k][r] = c + r < dim ? x[k][r] - mean0 : 0.0f;
-                    two[0] += x[k][r];
-                    two[1] = __builtin_fmaf(x[k][r], x[k][r], two[1]);
-                }
+            for (int e = 0; e < E; ++e) {
+                x[e] = c.valid(e) ? x[e] - mean0 : 0.0f;
+                two[0] += x[e];
+                two[1] = __builtin_fmaf(x[e], x[e], two[1]);
             }
             team_sum<TEAM, 2>(two, scratch + 16);
             const float delta = two[0] * rn;
             float var = two[1] * rn - delta * delta;
             var = var < 0.0f ? 0.0f : var;
             const float rstd = 1.0f / sqrtf(var + a.g.eps);
-            const bool some = begin != end;
             float gs[2] = {0.0f, 0.0f};
+            float w[E];
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int64_t c = c0 + k * stride;
-                float w[V];
+            for (int e = 0; e < E; ++e)
+                w[e] = 1.0f;
+            if (a.g.weight)
+                load_floats<WT, V, K, TAIL>(c, a.g.weight, w);
 #pragma unroll
-                for (int r = 0; r < V; ++r)
-                    w[r] = 1.0f;
-                if (a.g.weight)
-                    load_cols<WT, V>(a.g.weight, c, dim, w);
-#pragma unroll
-                for (int r = 0; r < V; ++r) {
-                    x[k][r] = (x[k][r] - delta) * rstd;
-                    if (some)
-                        dw[k][r] = __builtin_fmaf(s[k][r], x[k][r], dw[k][r]);
-                    db[k][r] += s[k][r];
-                    s[k][r] *= w[r];
-                    gs[0] += s[k][r];
-                    gs[1] = __builtin_fmaf(s[k][r], x[k][r], gs[1]);
-                }
+            for (int e = 0; e < E; ++e) {
+                x[e] = (x[e] - delta) * rstd;
+                if (some)
+                    dw[e] = __builtin_fmaf(s[e], x[e], dw[e]);
+                db[e] += s[e];
+                s[e] *= w[e];
+                gs[0] += s[e];
+                gs[1] = __builtin_fmaf(s[e], x[e], gs[1]);
             }
             team_sum<TEAM, 2>(gs, scratch + 48);
             const float c1 = gs[0] * rn, c2 = gs[1] * rn;
-            if (exists) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    float d[V];
-#pragma unroll
-                    for (int r = 0; r < V; ++r)
-                        d[r] = padding || !some
-                                   ? 0.0f
-                                   : rstd * __builtin_fmaf(-x[k][r], c2, s[k][r] - c1);
-                    store_cols<WT, V>(to, c0 + k * stride, dim, d);
-                }
-            }
+            for (int e = 0; e < E; ++e)
+                s[e] = padding || !some ? 0.0f : rstd * __builtin_fmaf(-x[e], c2, s[e] - c1);
+            if (exists)
+                store_row<WT>(c, to, s);
         }
     }
     if constexpr (STABLE) {
-        if (!a.partials)
-            return;
-        float *const out = a.partials + (int64_t)blockIdx.x * 2 * dim;
-        if constexpr (TEAM == kTeamGroup) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                store_cols<kF32, V>(out, c0 + k * stride, dim, dw[k]);
-                store_cols<kF32, V>(out + dim, c0 + k * stride, dim, db[k]);
-            }
-        } else {
-            // the teams' sums, in order (K is 1)
-            __shared__ float join[2][256 * V];
-#pragma unroll
-            for (int r = 0; r < V; ++r) {
-                join[0][threadIdx.x * V + r] = dw[0][r];
-                join[1][threadIdx.x * V + r] = db[0][r];
-            }
-            __syncthreads();
-            for (int64_t c = threadIdx.x; c < 2 * dim; c += 256) {
-                const int which = c >= dim, col = (int)(c - which * dim);
-                float t = join[which][col];
-                for (int i = 1; i < kTeams; ++i)
-                    t += join[which][i * (256 / kTeams) * V + col];
-                out[c] = t;
-            }
-        }
+        if (a.partials)
+            leave_partials<TEAM>(c, dw, db, dim, a.partials + (int64_t)blockIdx.x * 2 * dim);
     }
 }
 
@@ -591,19 +532,37 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     return l;
 }
 
+// Slabs of `slab` columns (a multiple of a vector) of the row's whole vectors; at least
+// one, for the elements behind them.
+template <int V>
+unsigned slabs_of(int64_t dim, int64_t slab)
+{
+    const int64_t n = (dim / V * V + slab - 1) / slab;
+    return (unsigned)(n < 1 ? 1 : n);
+}
+
 template <int WT, int YT, int TEAM, int K, bool STABLE>
 int64_t rows_k(const GradArgs &a, int threads, hipStream_t stream)
 {
     constexpr int V = vec_of<WT, YT>;
-    constexpr int kTeams = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
-    const int64_t slab = (int64_t)threads / kTeams * K * V;
+    constexpr int kTeams = teams_of<TEAM>;
     const int64_t most = STABLE ? kStableGroups : kRowGroups;
     int64_t groups = (a.g.num + kTeams - 1) / kTeams;
     groups = groups < most ? groups : most;
-    hipLaunchKernelGGL((rows_kernel<WT, YT, TEAM, K, STABLE>),
-                       dim3((unsigned)groups, (unsigned)((a.g.dim + slab - 1) / slab)),
-                       dim3((unsigned)threads), 0, stream, a);
+    const dim3 grid((unsigned)groups, slabs_of<V>(a.g.dim, (int64_t)threads / kTeams * K * V));
+    const dim3 block((unsigned)threads);
+    if (a.g.dim % V == 0)
+        hipLaunchKernelGGL((rows_kernel<WT, YT, TEAM, K, STABLE, false>), grid, block, 0, stream,
+                           a);
+    else
+        hipLaunchKernelGGL((rows_kernel<WT, YT, TEAM, K, STABLE, true>), grid, block, 0, stream, a);
     return groups;
+}
+
+// Threads of a group team for rows of `vectors` vectors, K to a lane.
+int threads_of(int64_t vectors, int k = 1)
+{
+    return (int)((vectors + 64 * k - 1) / (64 * k) * 64);
 }
 
 // The team that holds a row, and the launch; returns the workgroups.
@@ -611,18 +570,47 @@ template <int WT, int YT, bool STABLE>
 int64_t rows(const GradArgs &a, hipStream_t stream)
 {
     constexpr int V = vec_of<WT, YT>;
-    const int64_t vectors = (a.g.dim + V - 1) / V;
+    const int64_t vectors = a.g.dim / V;
     if (vectors <= 16)
         return rows_k<WT, YT, kTeam16, 1, STABLE>(a, 256, stream);
     if (vectors <= 64)
         return rows_k<WT, YT, kTeamWave, 1, STABLE>(a, 256, stream);
     if (vectors <= 1024)
-        return rows_k<WT, YT, kTeamGroup, 1, STABLE>(a, (int)((vectors + 63) / 64 * 64), stream);
+        return rows_k<WT, YT, kTeamGroup, 1, STABLE>(a, threads_of(vectors), stream);
     if constexpr (STABLE && V == 4) {
         if (vectors > 2048)
             return rows_k<WT, YT, kTeamGroup, 4, STABLE>(a, 1024, stream);
     }
     return rows_k<WT, YT, kTeamGroup, 2, STABLE>(a, 1024, stream);
+}
+
+template <int WT, int YT, int TEAM>
+void lookup_k(const LookupArgs &a, int threads, hipStream_t stream)
+{
+    constexpr int V = vec_of<WT, YT>;
+    const int64_t per = teams_of<TEAM> * kLookups;
+    const int64_t groups = (a.count + per - 1) / per;
+    const dim3 grid((unsigned)(groups < (1 << 16) ? groups : (1 << 16)),
+                    slabs_of<V>(a.dim, (int64_t)threads / teams_of<TEAM> * V));
+    if (a.dim % V == 0)
+        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, false>), grid, dim3((unsigned)threads), 0,
+                           stream, a);
+    else
+        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, true>), grid, dim3((unsigned)threads), 0,
+                           stream, a);
+}
+
+template <int WT, int YT>
+hipError_t lookup(const LookupArgs &a, hipStream_t stream)
+{
+    const int64_t vectors = a.dim / vec_of<WT, YT>;
+    if (vectors <= 16)
+        lookup_k<WT, YT, kTeam16>(a, 256, stream);
+    else if (vectors <= 64)
+        lookup_k<WT, YT, kTeamWave>(a, 256, stream);
+    else
+        lookup_k<WT, YT, kTeamGroup>(a, vectors < 512 ? threads_of(vectors) : 512, stream);
+    return hipGetLastError();
 }
 
 template <int WT, int YT>
@@ -691,19 +679,11 @@ int64_t lookup_workspace_bytes(int64_t count, int64_t num, int64_t dim, bool sta
 
 hipError_t launch_lookup(int wt, int yt, const LookupArgs &a, hipStream_t stream)
 {
-    const int64_t groups = (a.count + 3) / 4;
-    const dim3 grid((unsigned)(groups < (1 << 20) ? groups : (1 << 20))), block(256);
-    if (wt == kF32 && yt == kF32)
-        hipLaunchKernelGGL((lookup_kernel<kF32, kF32>), grid, block, 0, stream, a);
-    else if (wt == kF32 && yt == kF16)
-        hipLaunchKernelGGL((lookup_kernel<kF32, kF16>), grid, block, 0, stream, a);
-    else if (wt == kF32)
-        hipLaunchKernelGGL((lookup_kernel<kF32, kBF16>), grid, block, 0, stream, a);
-    else if (wt == kF16)
-        hipLaunchKernelGGL((lookup_kernel<kF16, kF16>), grid, block, 0, stream, a);
-    else
-        hipLaunchKernelGGL((lookup_kernel<kBF16, kBF16>), grid, block, 0, stream, a);
-    return hipGetLastError();
+    if (wt == kF32 && yt == kF32) return lookup<kF32, kF32>(a, stream);
+    if (wt == kF32 && yt == kF16) return lookup<kF32, kF16>(a, stream);
+    if (wt == kF32) return lookup<kF32, kBF16>(a, stream);
+    if (wt == kF16) return lookup<kF16, kF16>(a, stream);
+    return lookup<kBF16, kBF16>(a, stream);
 }
 
 hipError_t launch_lookup_backward(int wt, int yt, const LookupGradArgs &a, hipStream_t stream)

@@ -24,92 +24,107 @@ constexpr int vec_of = (elem_bytes<A> == 4 || elem_bytes<B> == 4) ? 4 : 8;
 constexpr float kNaN = __builtin_nanf("");
 
 // ---------------------------------------------------------------------------
-// Forward.  WAVES waves hold one row in registers, K vectors of V elements per
-// lane; with one wave per row a workgroup takes four rows.
+// Forward.  A team takes R consecutive rows at a time, K vectors of V elements per lane
+// and row, so that R rows' loads are in flight and their sums share a barrier; it keeps
+// its columns of the parameters in registers and walks the rows with the grid.
 // ---------------------------------------------------------------------------
 
-template <int WAVES>
-constexpr int rows_per_group = WAVES == 1 ? 4 : 1;
-template <int WAVES>
-constexpr int group_threads = WAVES == 1 ? 256 : 64 * WAVES;
-
-template <int XT, int PT, int YT, bool GATHER, int WAVES, int K>
-__global__ __launch_bounds__(group_threads<WAVES>) void norm_forward_kernel(const NormArgs a)
+template <int XT, int PT, int YT, bool GATHER, int TEAM, int K, int R, bool TAIL>
+__global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const NormArgs a)
 {
     constexpr int V = vec_of<XT, YT>;
-    __shared__ float scratch[3 * WAVES];
-    const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int kTeams = teams_of<TEAM>;
+    using C = Cols<V, K, TAIL>;
+    constexpr int E = C::kElems;
+    __shared__ float scratch[TEAM == kTeamGroup ? 3 * R * 16 : 1];
+    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
+    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t n = a.cols;
-    // (a second row's sums go to scratch behind a barrier that follows their reading)
-    for (int64_t row = (int64_t)blockIdx.x * rows_per_group<WAVES> +
-                       (WAVES == 1 ? threadIdx.x >> 6 : 0);
-         row < a.rows; row += (int64_t)gridDim.x * rows_per_group<WAVES>) {
-        int64_t from = row;
-        bool known = true;
-        if constexpr (GATHER) {
-            from = id_at(a.ids, row, a.ids64);
-            known = from >= 0 && from < a.table_rows;
-            if (!known)
-                from = 0;
+    const C c(n, lane, lanes);
+    const float rn = 1.0f / (float)n;
+    RawRow<PT, V, K, TAIL> pw, pb;
+    if (a.weight)
+        load_row<PT, false>(c, a.weight, pw);
+    if (a.bias)
+        load_row<PT, false>(c, a.bias, pb);
+    // (all of a workgroup's rounds are its teams' rounds, for the sums over a wave; a
+    // round's sums go to scratch behind a barrier that follows their last reading)
+    for (int64_t group = blockIdx.x; group * (kTeams * R) < a.rows; group += gridDim.x) {
+        const int64_t row0 = (group * kTeams + team) * R;
+        RawRow<XT, V, K, TAIL> raw[R];
+        int64_t from[R];
+        bool known[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            from[j] = row0 + j < a.rows ? row0 + j : a.rows - 1;
+            if constexpr (GATHER)
+                from[j] = id_at(a.ids, from[j], a.ids64);
         }
-        const void *const xp = row_of<XT>(a.x, from, a.x_stride);
-        float x[K][V];
-        float sum[1] = {0.0f};
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            load_cols<XT, V>(xp, (int64_t)(k * 64 * WAVES + lane) * V, n, x[k]);
-        const float rn = 1.0f / (float)n;
+        for (int j = 0; j < R; ++j) {
+            known[j] = true;
+            if constexpr (GATHER) {
+                known[j] = from[j] >= 0 && from[j] < a.table_rows;
+                from[j] = known[j] ? from[j] : 0;
+            }
+            load_row<XT, !GATHER>(c, row_of<XT>(a.x, from[j], a.x_stride), raw[j]);
+        }
+        float x[R][E];
+        float sum[R];
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int j = 0; j < R; ++j) {
+            sum[j] = 0.0f;
+            unpack<XT, V, K, TAIL>(raw[j], x[j]);
 #pragma unroll
-            for (int r = 0; r < V; ++r)
-                sum[0] += x[k][r];
-        group_sum<1, WAVES>(sum, scratch);
-        const float mean0 = sum[0] * rn;
-        float two[2] = {0.0f, 0.0f};
+            for (int e = 0; e < E; ++e)
+                sum[j] += x[j][e];
+        }
+        team_sum<TEAM, R>(sum, scratch);
+        float two[2 * R];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
+        for (int j = 0; j < R; ++j) {
+            const float mean0 = sum[j] * rn;
+            two[2 * j] = two[2 * j + 1] = 0.0f;
 #pragma unroll
-            for (int r = 0; r < V; ++r) {
-                x[k][r] = c + r < n ? x[k][r] - mean0 : 0.0f;
-                two[0] += x[k][r];
-                two[1] = __builtin_fmaf(x[k][r], x[k][r], two[1]);
+            for (int e = 0; e < E; ++e) {
+                x[j][e] = c.valid(e) ? x[j][e] - mean0 : 0.0f;
+                two[2 * j] += x[j][e];
+                two[2 * j + 1] = __builtin_fmaf(x[j][e], x[j][e], two[2 * j + 1]);
             }
         }
-        group_sum<2, WAVES>(two, scratch + WAVES);
-        const float delta = two[0] * rn;
-        float var = two[1] * rn - delta * delta;
-        var = var < 0.0f ? 0.0f : var;
-        const float rstd = 1.0f / sqrtf(var + a.eps);
-        if (a.mean && lane == 0) {
-            a.mean[row] = mean0 + delta;
-            a.rstd[row] = rstd;
-        }
-        void *const yp = row_of<YT>(a.y, row, n);
+        team_sum<TEAM, 2 * R>(two, scratch + R * 16);
+        float w[E], b[E];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
-            if (c >= n)
+        for (int e = 0; e < E; ++e) {
+            w[e] = 1.0f;
+            b[e] = 0.0f;
+        }
+        if (a.weight)
+            unpack<PT, V, K, TAIL>(pw, w);
+        if (a.bias)
+            unpack<PT, V, K, TAIL>(pb, b);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = row0 + j;
+            if (row >= a.rows)
                 break;
-            float w[V], b[V];
-#pragma unroll
-            for (int r = 0; r < V; ++r) {
-                w[r] = 1.0f;
-                b[r] = 0.0f;
+            const float delta = two[2 * j] * rn;
+            float var = two[2 * j + 1] * rn - delta * delta;
+            var = var < 0.0f ? 0.0f : var;
+            const float rstd = 1.0f / sqrtf(var + a.eps);
+            if (a.mean && lane == 0) {
+                a.mean[row] = sum[j] * rn + delta;
+                a.rstd[row] = rstd;
             }
-            if (a.weight)
-                load_cols<PT, V>(a.weight, c, n, w);
-            if (a.bias)
-                load_cols<PT, V>(a.bias, c, n, b);
-            float y[V];
+            float y[E];
 #pragma unroll
-            for (int r = 0; r < V; ++r) {
-                y[r] = __builtin_fmaf((x[k][r] - delta) * rstd, w[r], b[r]);
-                if (GATHER && !known)
-                    y[r] = kNaN;
+            for (int e = 0; e < E; ++e) {
+                y[e] = __builtin_fmaf((x[j][e] - delta) * rstd, w[e], b[e]);
+                if (GATHER && !known[j])
+                    y[e] = kNaN;
             }
-            store_cols<YT, V>(yp, c, n, y);
+            store_row<YT>(c, row_of<YT>(a.y, row, n), y);
         }
     }
 }
@@ -121,7 +136,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
 {
     constexpr int V = vec_of<XT, YT>;
     constexpr int64_t kStep = (int64_t)64 * kLongWaves * V;
-    __shared__ float scratch[3 * kLongWaves];
+    __shared__ float scratch[3 * 16];
     const int64_t n = a.cols;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         int64_t from = row;
@@ -143,7 +158,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
             for (int r = 0; r < V; ++r)
                 sum[0] += x[r];
         }
-        group_sum<1, kLongWaves>(sum, scratch);
+        team_sum<kTeamGroup, 1>(sum, scratch);
         const float mean0 = sum[0] * rn;
         float two[2] = {0.0f, 0.0f};
         for (int64_t c = c0; c < n; c += kStep) {
@@ -156,7 +171,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
                 two[1] = __builtin_fmaf(d, d, two[1]);
             }
         }
-        group_sum<2, kLongWaves>(two, scratch + kLongWaves);
+        team_sum<kTeamGroup, 2>(two, scratch + 16);
         const float delta = two[0] * rn;
         float var = two[1] * rn - delta * delta;
         var = var < 0.0f ? 0.0f : var;
@@ -189,149 +204,136 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
     }
 }
 
-// A workgroup per row (or four), within the limit of 2^32 work-items of a launch.
-unsigned forward_groups(int64_t rows, int per_group)
+template <int XT, int PT, int YT, bool GATHER, int TEAM, int K, int R>
+void forward_k(const NormArgs &a, int threads, hipStream_t stream)
 {
-    const int64_t groups = (rows + per_group - 1) / per_group;
-    return (unsigned)(groups < (1 << 20) ? groups : (1 << 20));
+    constexpr int V = vec_of<XT, YT>;
+    const int64_t rows = teams_of<TEAM> * R;
+    const int64_t groups = (a.rows + rows - 1) / rows;
+    const int64_t most = 2048 * 256 / threads;
+    const dim3 grid((unsigned)(groups < most ? groups : most)), block((unsigned)threads);
+    if (a.cols % V == 0)
+        hipLaunchKernelGGL((norm_forward_kernel<XT, PT, YT, GATHER, TEAM, K, R, false>), grid,
+                           block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((norm_forward_kernel<XT, PT, YT, GATHER, TEAM, K, R, true>), grid,
+                           block, 0, stream, a);
 }
 
-template <int XT, int PT, int YT, bool GATHER, int WAVES, int K>
-void forward_k(const NormArgs &a, hipStream_t stream)
+// Threads of a group team for rows of `vectors` vectors, K to a lane (at least a wave: a
+// row's last elements, fewer than a vector, take a lane each).
+int threads_of(int64_t vectors, int k = 1)
 {
-    hipLaunchKernelGGL((norm_forward_kernel<XT, PT, YT, GATHER, WAVES, K>),
-                       dim3(forward_groups(a.rows, rows_per_group<WAVES>)),
-                       dim3(group_threads<WAVES>), 0, stream, a);
+    return (int)((vectors + 64 * k - 1) / (64 * k) * 64);
 }
 
 template <int XT, int PT, int YT, bool GATHER>
 hipError_t forward(const NormArgs &a, hipStream_t stream)
 {
-    constexpr int64_t kWave = 64 * vec_of<XT, YT>;  // a wave's elements per vector
-    const int64_t k = (a.cols + kWave - 1) / kWave;
-    if (k <= 1)
-        forward_k<XT, PT, YT, GATHER, 1, 1>(a, stream);
-    else if (k <= 2)
-        forward_k<XT, PT, YT, GATHER, 1, 2>(a, stream);
-    else if (k <= 4)
-        forward_k<XT, PT, YT, GATHER, 1, 4>(a, stream);
-    else if (k <= 8)
-        forward_k<XT, PT, YT, GATHER, 1, 8>(a, stream);
-    else if (k <= 16)
-        forward_k<XT, PT, YT, GATHER, 4, 4>(a, stream);
-    else if (k <= 32)
-        forward_k<XT, PT, YT, GATHER, 4, 8>(a, stream);
-    else if (k <= 64)
-        forward_k<XT, PT, YT, GATHER, 16, 4>(a, stream);
+    constexpr int V = vec_of<XT, YT>;
+    const int64_t vectors = a.cols / V;
+    if (vectors <= 16)
+        forward_k<XT, PT, YT, GATHER, kTeam16, 1, 4>(a, 256, stream);
+    else if (vectors <= 64)
+        forward_k<XT, PT, YT, GATHER, kTeamWave, 1, 4>(a, 256, stream);
+    else if (vectors <= 512)
+        forward_k<XT, PT, YT, GATHER, kTeamGroup, 1, 4>(a, threads_of(vectors), stream);
+    else if (vectors <= 1024)
+        forward_k<XT, PT, YT, GATHER, kTeamGroup, 1, 2>(a, threads_of(vectors), stream);
+    else if (vectors <= 2048)
+        forward_k<XT, PT, YT, GATHER, kTeamGroup, 2, 1>(a, threads_of(vectors, 2), stream);
+    else if (vectors <= 4096)
+        forward_k<XT, PT, YT, GATHER, kTeamGroup, 4, 1>(a, threads_of(vectors, 4), stream);
     else
         hipLaunchKernelGGL((norm_forward_long_kernel<XT, PT, YT, GATHER>),
-                           dim3(forward_groups(a.rows, 1)), dim3(64 * kLongWaves), 0, stream, a);
+                           dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))),
+                           dim3(64 * kLongWaves), 0, stream, a);
     return hipGetLastError();
 }
 
+// Most workgroups of a backward pass of 256 threads each (four per CU).
+constexpr int64_t kNormGradGroups = 1024;
+
 // ---------------------------------------------------------------------------
-// Backward.  Workgroups walk the rows; each keeps the sums of dy xh and dy of its
-// rows per column in registers and leaves them in the workspace.
+// Backward.  As the forward pass; each workgroup also keeps the sums of dy xh and dy of
+// its rows per column in registers and leaves them in the workspace.
 // ---------------------------------------------------------------------------
 
-template <int XT, int PT, int WAVES, int K>
-__global__ __launch_bounds__(group_threads<WAVES>) void norm_backward_kernel(const NormGradArgs a)
+template <int XT, int PT, int TEAM, int K, int R, bool TAIL>
+__global__ __launch_bounds__(most_threads<TEAM>) void norm_backward_kernel(const NormGradArgs a)
 {
     constexpr int V = vec_of<XT, XT>;
-    constexpr int kTeams = rows_per_group<WAVES>;
-    __shared__ float scratch[4 * WAVES];
-    const int team = WAVES == 1 ? threadIdx.x >> 6 : 0;
-    const int lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int kTeams = teams_of<TEAM>;
+    using C = Cols<V, K, TAIL>;
+    constexpr int E = C::kElems;
+    __shared__ float scratch[TEAM == kTeamGroup ? 2 * 2 * R * 16 : 1];
+    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
+    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t n = a.cols;
+    const C c(n, lane, lanes);
     const float rn = 1.0f / (float)n;
-    float w[K][V], dw[K][V], db[K][V];
+    float w[E], dw[E], db[E];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-#pragma unroll
-        for (int r = 0; r < V; ++r) {
-            w[k][r] = 1.0f;
-            dw[k][r] = 0.0f;
-            db[k][r] = 0.0f;
-        }
-        if (a.weight)
-            load_cols<PT, V>(a.weight, (int64_t)(k * 64 * WAVES + lane) * V, n, w[k]);
+    for (int e = 0; e < E; ++e) {
+        w[e] = 1.0f;
+        dw[e] = db[e] = 0.0f;
     }
-    for (int64_t row = (int64_t)blockIdx.x * kTeams + team; row < a.rows;
-         row += (int64_t)gridDim.x * kTeams) {
-        const void *const xp = row_of<XT>(a.x, row, a.x_stride);
-        const void *const gp = row_of<XT>(a.dy, row, a.dy_stride);
-        const float mean = G(a.mean)[row], rstd = G(a.rstd)[row];
-        float x[K][V], dy[K][V];
-        float two[2] = {0.0f, 0.0f};
+    if (a.weight)
+        load_floats<PT, V, K, TAIL>(c, a.weight, w);
+    int side = 0;  // two rounds' sums take turns in scratch
+    for (int64_t group = blockIdx.x; group * (kTeams * R) < a.rows; group += gridDim.x) {
+        const int64_t row0 = (group * kTeams + team) * R;
+        RawRow<XT, V, K, TAIL> rx[R], rg[R];
+        float mean[R], rstd[R];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
-            load_cols<XT, V>(xp, c, n, x[k], mean);
-            load_cols<XT, V>(gp, c, n, dy[k]);
+        for (int j = 0; j < R; ++j) {
+            const int64_t row = row0 + j < a.rows ? row0 + j : a.rows - 1;
+            load_row<XT, true>(c, row_of<XT>(a.x, row, a.x_stride), rx[j]);
+            load_row<XT, true>(c, row_of<XT>(a.dy, row, a.dy_stride), rg[j]);
+            mean[j] = G(a.mean)[row];
+            rstd[j] = G(a.rstd)[row];
         }
+        // behind the row's end dy is 0, and so is everything that is summed
+        float x[R][E], dy[R][E];
+        float two[2 * R];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
+        for (int j = 0; j < R; ++j) {
+            const bool live = row0 + j < a.rows;
+            two[2 * j] = two[2 * j + 1] = 0.0f;
+            unpack<XT, V, K, TAIL>(rx[j], x[j]);
+            unpack<XT, V, K, TAIL>(rg[j], dy[j]);
 #pragma unroll
-            for (int r = 0; r < V; ++r) {
-                x[k][r] = (x[k][r] - mean) * rstd;
-                dw[k][r] = __builtin_fmaf(dy[k][r], x[k][r], dw[k][r]);
-                db[k][r] += dy[k][r];
-                dy[k][r] *= w[k][r];
-                two[0] += dy[k][r];
-                two[1] = __builtin_fmaf(dy[k][r], x[k][r], two[1]);
-            }
-        }
-        if (a.dx) {
-            if constexpr (WAVES > 1)
-                __syncthreads();  // the previous row's sums have been read
-            group_sum<2, WAVES>(two, scratch);
-            const float c1 = two[0] * rn, c2 = two[1] * rn;
-            void *const dp = row_of<XT>(a.dx, row, n);
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float d[V];
-#pragma unroll
-                for (int r = 0; r < V; ++r)
-                    d[r] = rstd * __builtin_fmaf(-x[k][r], c2, dy[k][r] - c1);
-                store_cols<XT, V>(dp, (int64_t)(k * 64 * WAVES + lane) * V, n, d);
-            }
-        }
-    }
-    if (!a.partials)
-        return;
-    float *const out = a.partials + (int64_t)blockIdx.x * 2 * n;
-    if constexpr (kTeams == 1) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int64_t c = (int64_t)(k * 64 * WAVES + lane) * V;
-            store_cols<kF32, V>(out, c, n, dw[k]);
-            store_cols<kF32, V>(out + n, c, n, db[k]);
-        }
-    } else {
-        // the teams' sums, in order
-        __shared__ float join[kTeams][2][64 * V];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            __syncthreads();
-#pragma unroll
-            for (int r = 0; r < V; ++r) {
-                join[team][0][r * 64 + lane] = dw[k][r];
-                join[team][1][r * 64 + lane] = db[k][r];
-            }
-            __syncthreads();
-            if (team < 2) {
-                float s[V];
-#pragma unroll
-                for (int r = 0; r < V; ++r) {
-                    s[r] = join[0][team][r * 64 + lane];
-#pragma unroll
-                    for (int t = 1; t < kTeams; ++t)
-                        s[r] += join[t][team][r * 64 + lane];
+            for (int e = 0; e < E; ++e) {
+                x[j][e] = (x[j][e] - mean[j]) * rstd[j];
+                if (live) {
+                    dw[e] = __builtin_fmaf(dy[j][e], x[j][e], dw[e]);
+                    db[e] += dy[j][e];
                 }
-                store_cols<kF32, V>(out + team * n, (int64_t)(k * 64 + lane) * V, n, s);
+                dy[j][e] *= w[e];
+                two[2 * j] += dy[j][e];
+                two[2 * j + 1] = __builtin_fmaf(dy[j][e], x[j][e], two[2 * j + 1]);
             }
         }
+        if (!a.dx)
+            continue;
+        team_sum<TEAM, 2 * R>(two, scratch + side);
+        if constexpr (TEAM == kTeamGroup)
+            side = 2 * R * 16 - side;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            if (row0 + j >= a.rows)
+                break;
+            const float c1 = two[2 * j] * rn, c2 = two[2 * j + 1] * rn;
+            float d[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                d[e] = rstd[j] * __builtin_fmaf(-x[j][e], c2, dy[j][e] - c1);
+            store_row<XT>(c, row_of<XT>(a.dx, row0 + j, n), d);
+        }
     }
+    if (a.partials)
+        leave_partials<TEAM>(c, dw, db, n, a.partials + (int64_t)blockIdx.x * 2 * n);
 }
 
 // Rows too long for registers: the row is read twice, and the parameters' gradients
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_backward_long_kernel(con
 {
     constexpr int V = vec_of<XT, XT>;
     constexpr int64_t kStep = (int64_t)64 * kLongWaves * V;
-    __shared__ float scratch[2 * kLongWaves];
+    __shared__ float scratch[2 * 16];
     const int64_t n = a.cols;
     const int64_t c0 = (int64_t)threadIdx.x * V;
     const float rn = 1.0f / (float)n;
@@ -386,7 +388,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_backward_long_kernel(con
         if (!a.dx)
             continue;
         __syncthreads();  // the previous row's sums have been read
-        group_sum<2, kLongWaves>(two, scratch);
+        team_sum<kTeamGroup, 2>(two, scratch);
         const float c1 = two[0] * rn, c2 = two[1] * rn;
         void *const dp = row_of<XT>(a.dx, row, n);
         for (int64_t c = c0; c < n; c += kStep) {
@@ -406,34 +408,40 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_backward_long_kernel(con
     }
 }
 
-template <int XT, int PT, int WAVES, int K>
-void backward_k(const NormGradArgs &a, hipStream_t stream)
+template <int XT, int PT, int TEAM, int K, int R>
+int64_t backward_k(const NormGradArgs &a, int threads, hipStream_t stream)
 {
-    hipLaunchKernelGGL((norm_backward_kernel<XT, PT, WAVES, K>), dim3((unsigned)a.groups),
-                       dim3(group_threads<WAVES>), 0, stream, a);
+    const int64_t rows = teams_of<TEAM> * R;
+    int64_t groups = (a.rows + rows - 1) / rows;
+    const int64_t most = kNormGradGroups * 256 / (threads < 256 ? 256 : threads);
+    groups = groups < most ? groups : most;
+    const dim3 grid((unsigned)groups), block((unsigned)threads);
+    if (a.cols % vec_of<XT, XT> == 0)
+        hipLaunchKernelGGL((norm_backward_kernel<XT, PT, TEAM, K, R, false>), grid, block, 0,
+                           stream, a);
+    else
+        hipLaunchKernelGGL((norm_backward_kernel<XT, PT, TEAM, K, R, true>), grid, block, 0,
+                           stream, a);
+    return groups;
 }
 
 template <int XT, int PT>
-hipError_t backward(const NormGradArgs &a, hipStream_t stream)
+int64_t backward(const NormGradArgs &a, hipStream_t stream)
 {
-    constexpr int64_t kWave = 64 * vec_of<XT, XT>;
-    const int64_t k = (a.cols + kWave - 1) / kWave;
-    if (k <= 1)
-        backward_k<XT, PT, 1, 1>(a, stream);
-    else if (k <= 2)
-        backward_k<XT, PT, 1, 2>(a, stream);
-    else if (k <= 4)
-        backward_k<XT, PT, 1, 4>(a, stream);
-    else if (k <= 8)
-        backward_k<XT, PT, 4, 2>(a, stream);
-    else if (k <= 16)
-        backward_k<XT, PT, 4, 4>(a, stream);
-    else if (k <= 32)
-        backward_k<XT, PT, 16, 2>(a, stream);
-    else
-        hipLaunchKernelGGL((norm_backward_long_kernel<XT, PT>), dim3((unsigned)a.groups),
-                           dim3(64 * kLongWaves), 0, stream, a);
-    return hipGetLastError();
+    constexpr int V = vec_of<XT, XT>;
+    const int64_t vectors = a.cols / V;
+    if (vectors <= 16)
+        return backward_k<XT, PT, kTeam16, 1, 2>(a, 256, stream);
+    if (vectors <= 64)
+        return backward_k<XT, PT, kTeamWave, 1, 2>(a, 256, stream);
+    if (vectors <= 1024)
+        return backward_k<XT, PT, kTeamGroup, 1, 2>(a, threads_of(vectors), stream);
+    if (vectors <= 2048)
+        return backward_k<XT, PT, kTeamGroup, 2, 1>(a, threads_of(vectors, 2), stream);
+    const int64_t groups = a.rows < 512 ? a.rows : 512;
+    hipLaunchKernelGGL((norm_backward_long_kernel<XT, PT>), dim3((unsigned)groups),
+                       dim3(64 * kLongWaves), 0, stream, a);
+    return groups;
 }
 
 // Sums of the partials over the groups: one workgroup per 64 columns of one of the two
@@ -467,12 +475,10 @@ __global__ __launch_bounds__(64 * kSumWaves) void param_grads_kernel(const float
 
 }  // namespace
 
-// Workgroups of the backward pass: two per CU hold the registers of the longest rows
-// in flight; each leaves 8 bytes per column in the workspace.
-int64_t norm_grad_groups(int64_t rows, int64_t cols)
+int64_t norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    (void)cols;
-    return rows < 512 ? (rows < 1 ? 1 : rows) : 512;
+    const int64_t groups = rows < 1 ? 1 : rows < kNormGradGroups ? rows : kNormGradGroups;
+    return groups * 2 * cols * 4;
 }
 
 hipError_t launch_norm_forward(int xt, int pt, int yt, const NormArgs &a, hipStream_t stream)
@@ -510,20 +516,22 @@ hipError_t launch_param_grads(int pt, const float *partials, int64_t groups, int
 
 hipError_t launch_norm_backward(int xt, int pt, const NormGradArgs &a, hipStream_t stream)
 {
-    hipError_t e;
-    if (a.rows == 0) {
-        e = hipSuccess;
-    } else if (xt == kF32) {
-        e = backward<kF32, kF32>(a, stream);
-    } else if (xt == kF16) {
-        e = pt == kF32 ? backward<kF16, kF32>(a, stream) : backward<kF16, kF16>(a, stream);
-    } else {
-        e = pt == kF32 ? backward<kBF16, kF32>(a, stream) : backward<kBF16, kBF16>(a, stream);
+    int64_t groups = 0;
+    if (a.rows > 0) {
+        if (xt == kF32)
+            groups = backward<kF32, kF32>(a, stream);
+        else if (xt == kF16)
+            groups = pt == kF32 ? backward<kF16, kF32>(a, stream) : backward<kF16, kF16>(a, stream);
+        else
+            groups = pt == kF32 ? backward<kBF16, kF32>(a, stream)
+                                : backward<kBF16, kBF16>(a, stream);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess)
+            return e;
     }
-    if (e != hipSuccess || !a.partials)
-        return e;
-    return launch_param_grads(pt, a.partials, a.rows == 0 ? 0 : a.groups, a.cols, a.dweight,
-                              a.dbias, stream);
+    if (!a.partials)
+        return hipSuccess;
+    return launch_param_grads(pt, a.partials, groups, a.cols, a.dweight, a.dbias, stream);
 }
 
 }  // namespace bq

@@ -40,13 +40,10 @@ struct NormGradArgs {
     void *dx;            // may be null; rows packed
     void *dweight;       // may be null
     void *dbias;         // may be null
-    float *partials;     // norm_grad_groups() x 2 x cols
+    float *partials;     // of every workgroup [2][cols]: its rows' part of the two
     int64_t rows, cols, dy_stride, x_stride;
-    int32_t groups;
 };
-// Workgroups of the backward pass: each adds up the parameters' gradients of its
-// rows and leaves them in the workspace.
-int64_t norm_grad_groups(int64_t rows, int64_t cols);
+int64_t norm_workspace_bytes(int64_t rows, int64_t cols);
 hipError_t launch_norm_backward(int xt, int pt, const NormGradArgs &a, hipStream_t stream);
 
 // The sums over `groups` partial rows [2][cols] (the parameters' gradients), in

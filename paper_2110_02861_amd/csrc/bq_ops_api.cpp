@@ -24,6 +24,7 @@ bq_status from_hip(hipError_t e) { return e == hipSuccess ? BQ_OK : BQ_ERR_HIP; 
 // Byte offsets stay far below 2^63, and a row's length below 2^31.
 constexpr int64_t kMaxRows = int64_t{1} << 40;
 constexpr int64_t kMaxCols = int64_t{1} << 30;
+constexpr int64_t kMaxDim = int64_t{1} << 24;  // at most 2^16 slabs of a launch
 
 bq_status check_norm(bq_dtype dtype, bq_dtype param_dtype, int64_t rows, int64_t cols, float eps)
 {
@@ -51,7 +52,7 @@ bq_status check_lookup(bq_dtype dtype, bq_dtype out_dtype, int64_t num, int64_t 
         (dtype != BQ_F32 && out_dtype != dtype) || (id_bits != 32 && id_bits != 64))
         return BQ_ERR_DTYPE;
     if (count < 0 || num < 1 || dim < 1 || count > INT32_MAX || num >= INT32_MAX ||
-        dim > kMaxCols)
+        dim > kMaxDim)
         return BQ_ERR_SIZE;
     return BQ_OK;
 }
@@ -97,7 +98,7 @@ int64_t bq_layer_norm_workspace_bytes(int64_t rows, int64_t cols)
 {
     if (rows < 0 || cols < 1 || rows > kMaxRows || cols > kMaxCols)
         return 0;
-    return bq::norm_grad_groups(rows, cols) * 2 * cols * 4;
+    return bq::norm_workspace_bytes(rows, cols);
 }
 
 bq_status bq_layer_norm_backward(bq_dtype dtype, bq_dtype param_dtype, const void *dy,
@@ -136,7 +137,6 @@ bq_status bq_layer_norm_backward(bq_dtype dtype, bq_dtype param_dtype, const voi
     a.cols = cols;
     a.dy_stride = dy_stride;
     a.x_stride = x_stride;
-    a.groups = static_cast<int32_t>(bq::norm_grad_groups(rows, cols));
     return from_hip(bq::launch_norm_backward(dtype, param_dtype, a, stream));
 }
 

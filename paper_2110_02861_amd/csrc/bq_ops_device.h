@@ -31,9 +31,13 @@ __device__ inline float load1(const void *p, int64_t i)
 __device__ inline uint32_t bits16(float lo, float hi, int dt)
 {
     // both roundings are to nearest, ties to even
-    if (dt == kF16)
+    if (dt == kF16) {
+        // the values as they are in fp32: a product would otherwise be rounded once, to
+        // fp16, where the compiler finds an instruction for it, and twice elsewhere
+        asm("" : "+v"(lo), "+v"(hi));
         return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) |
                (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16;
+    }
     return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)lo) |
            (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)hi) << 16;
 }
@@ -47,34 +51,63 @@ __device__ inline void store1(void *p, int64_t i, float v)
         G(static_cast<uint16_t *>(p))[i] = (uint16_t)bits16(v, 0.0f, DT);
 }
 
-// V elements (4 or 8) from element i on, as fp32.
+// V elements (4 or 8) as they are in memory.
+template <int DT, int V>
+struct Raw {
+    static_assert(V == 4 || V == 8, "vector length");
+    static constexpr int kWords = V * elem_bytes<DT> / 4;
+    uint32_t w[kWords];
+};
+
+template <int DT, int V>
+__device__ inline void unpack(const Raw<DT, V> &x, float (&o)[V])
+{
+#pragma unroll
+    for (int i = 0; i < Raw<DT, V>::kWords; ++i) {
+        if constexpr (DT == kF32) {
+            o[i] = __uint_as_float(x.w[i]);
+        } else {
+            o[2 * i] = g16_lo<DT>(x.w[i]);
+            o[2 * i + 1] = g16_hi<DT>(x.w[i]);
+        }
+    }
+}
+
+// From element i on, NT: with the non-temporal hint.
+template <int DT, int V, bool NT>
+__device__ inline Raw<DT, V> load_raw(const void *p, int64_t i)
+{
+    Raw<DT, V> x;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p) + i * elem_bytes<DT>;
+    if constexpr (Raw<DT, V>::kWords == 2) {
+        const gvu2_any2 q = (gvu2_any2)at;
+        const vu2 v = NT ? __builtin_nontemporal_load(q) : *q;
+        x.w[0] = v.x;
+        x.w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int h = 0; h < Raw<DT, V>::kWords / 4; ++h) {
+            vu4 v;
+            if constexpr (DT == kF32) {
+                const gvu4_any q = (gvu4_any)(at + 16 * h);
+                v = NT ? __builtin_nontemporal_load(q) : *q;
+            } else {
+                const gvu4_any2 q = (gvu4_any2)(at + 16 * h);
+                v = NT ? __builtin_nontemporal_load(q) : *q;
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                x.w[4 * h + r] = v[r];
+        }
+    }
+    return x;
+}
+
+// V elements from element i on, as fp32.
 template <int DT, int V>
 __device__ inline void load_vec(const void *p, int64_t i, float (&o)[V])
 {
-    static_assert(V == 4 || V == 8, "vector length");
-    if constexpr (DT == kF32) {
-#pragma unroll
-        for (int h = 0; h < V / 4; ++h) {
-            const vu4 w = *(gvu4_any)(uintptr_t)(static_cast<const float *>(p) + i + 4 * h);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                o[4 * h + r] = __uint_as_float(w[r]);
-        }
-    } else if constexpr (V == 8) {
-        const vu4 w = *(gvu4_any2)(uintptr_t)(static_cast<const uint16_t *>(p) + i);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            o[2 * r] = g16_lo<DT>(w[r]);
-            o[2 * r + 1] = g16_hi<DT>(w[r]);
-        }
-    } else {
-        const vu2 w = *(gvu2_any2)(uintptr_t)(static_cast<const uint16_t *>(p) + i);
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            o[2 * r] = g16_lo<DT>(w[r]);
-            o[2 * r + 1] = g16_hi<DT>(w[r]);
-        }
-    }
+    unpack<DT, V>(load_raw<DT, V, false>(p, i), o);
 }
 
 template <int DT, int V>
@@ -171,29 +204,177 @@ __device__ inline float wave_sum(float v)
     return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-// Sums of N values over WAVES waves, in every thread; scratch holds N * WAVES
-// floats.  Ends without a barrier: the next use of the same scratch needs one before.
-template <int N, int WAVES>
-__device__ inline void group_sum(float (&v)[N], float *scratch)
+// A team of lanes holds a row: 16 lanes (four teams to a wave), a wave (four to a
+// workgroup), or a workgroup of as many waves as the row needs.
+enum { kTeam16 = 0, kTeamWave = 1, kTeamGroup = 2 };
+template <int TEAM>
+constexpr int teams_of = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
+template <int TEAM>
+constexpr int most_threads = TEAM == kTeamGroup ? 1024 : 256;
+
+// Sums of N values over the team, in every lane; scratch (group teams): 16 floats per
+// value.  One barrier, before the results are read: the next use of the same scratch
+// needs another barrier before it.
+template <int TEAM, int N>
+__device__ inline void team_sum(float (&v)[N], float *scratch)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        v[i] = wave_sum(v[i]);
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x >> 6;
+    for (int i = 0; i < N; ++i) {
+        if constexpr (TEAM == kTeam16) {
+            v[i] = dpp_fadd<0xb1>(v[i]);
+            v[i] = dpp_fadd<0x4e>(v[i]);
+            v[i] = dpp_fadd<0x141>(v[i]);
+            v[i] = dpp_fadd<0x140>(v[i]);
+        } else {
+            v[i] = wave_sum(v[i]);
+        }
+    }
+    if constexpr (TEAM == kTeamGroup) {
+        const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                scratch[i * WAVES + wave] = v[i];
+                scratch[i * 16 + wave] = v[i];
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            float s = scratch[i * WAVES];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w)
-                s += scratch[i * WAVES + w];
+            float s = scratch[i * 16];
+            for (int w = 1; w < waves; ++w)
+                s += scratch[i * 16 + w];
             v[i] = s;
+        }
+    }
+}
+
+// The columns of a row of n that a lane of its team holds: K vectors of V elements,
+// `stride` columns apart, of the row's whole vectors, and with TAIL (n no multiple of V)
+// one of the fewer than V elements behind those.  Every access is a vector or an
+// element under one condition without an alternative: with one, lanes that are past the
+// row's end would write registers that loads of the others are still to fill, and wait
+// for each load in turn (32768 x 1600 in bf16: 71 us against 45).
+template <int V, int K, bool TAIL>
+struct Cols {
+    static constexpr int kElems = K * V + (TAIL ? 1 : 0);
+    uint32_t c0, stride, whole, tail;
+    bool has_tail;
+
+    __device__ Cols(int64_t n, int lane, int lanes, int64_t from = 0)
+    {
+        c0 = (uint32_t)(from + lane * V);
+        stride = (uint32_t)(lanes * V);
+        whole = (uint32_t)(n / V * V);
+        tail = whole + lane;
+        has_tail = TAIL && from == 0 && tail < (uint32_t)n;  // the first slab's
+    }
+    __device__ uint32_t col(int k) const { return c0 + k * stride; }
+    __device__ bool has(int k) const { return col(k) < whole; }
+    // whether element e of the lane is one of the row
+    __device__ bool valid(int e) const { return e < K * V ? has(e / V) : has_tail; }
+};
+
+template <int DT, int V, int K, bool TAIL>
+struct RawRow {
+    Raw<DT, V> v[K];
+    uint32_t t;
+};
+
+template <int DT, bool NT, int V, int K, bool TAIL>
+__device__ inline void load_row(const Cols<V, K, TAIL> &c, const void *row,
+                                RawRow<DT, V, K, TAIL> &x)
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int i = 0; i < Raw<DT, V>::kWords; ++i)
+            x.v[k].w[i] = 0;
+        if (c.has(k))
+            x.v[k] = load_raw<DT, V, NT>(row, c.col(k));
+    }
+    if constexpr (TAIL) {
+        x.t = 0;
+        if (c.has_tail) {
+            if constexpr (DT == kF32)
+                x.t = G(static_cast<const uint32_t *>(row))[c.tail];
+            else
+                x.t = G(static_cast<const uint16_t *>(row))[c.tail];
+        }
+    }
+}
+
+template <int DT, int V, int K, bool TAIL>
+__device__ inline void unpack(const RawRow<DT, V, K, TAIL> &x, float (&o)[K * V + (TAIL ? 1 : 0)])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[V];
+        unpack<DT, V>(x.v[k], f);
+#pragma unroll
+        for (int r = 0; r < V; ++r)
+            o[k * V + r] = f[r];
+    }
+    if constexpr (TAIL)
+        o[K * V] = DT == kF32 ? __uint_as_float(x.t) : g16_lo<DT>(x.t);
+}
+
+template <int DT, int V, int K, bool TAIL>
+__device__ inline void load_floats(const Cols<V, K, TAIL> &c, const void *row,
+                                   float (&o)[K * V + (TAIL ? 1 : 0)])
+{
+    RawRow<DT, V, K, TAIL> x;
+    load_row<DT, false>(c, row, x);
+    unpack<DT, V, K, TAIL>(x, o);
+}
+
+template <int DT, int V, int K, bool TAIL>
+__device__ inline void store_row(const Cols<V, K, TAIL> &c, void *row,
+                                 const float (&v)[K * V + (TAIL ? 1 : 0)])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        float f[V];
+#pragma unroll
+        for (int r = 0; r < V; ++r)
+            f[r] = v[k * V + r];
+        if (c.has(k))
+            store_vec<DT, V>(row, c.col(k), f);
+    }
+    if constexpr (TAIL) {
+        if (c.has_tail)
+            store1<DT>(row, c.tail, v[K * V]);
+    }
+}
+
+// Leaves a workgroup's sums per column of two gradients in out[2][n]: its only team's, or
+// (K == 1) its teams' in order.  All threads call it.
+template <int TEAM, int V, int K, bool TAIL>
+__device__ inline void leave_partials(const Cols<V, K, TAIL> &c,
+                                      const float (&dw)[K * V + (TAIL ? 1 : 0)],
+                                      const float (&db)[K * V + (TAIL ? 1 : 0)], int64_t n,
+                                      float *out)
+{
+    if constexpr (TEAM == kTeamGroup) {
+        store_row<kF32>(c, out, dw);
+        store_row<kF32>(c, out + n, db);
+    } else {
+        constexpr int kTeams = teams_of<TEAM>, kLanes = 256 / kTeams;
+        static_assert(K == 1, "a team of a wave or less holds one vector per lane");
+        constexpr int E = V + (TAIL ? 1 : 0);
+        __shared__ float join[2][E][256];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            join[0][e][threadIdx.x] = dw[e];
+            join[1][e][threadIdx.x] = db[e];
+        }
+        __syncthreads();
+        for (int64_t i = threadIdx.x; i < 2 * n; i += 256) {
+            const int which = i >= n, col = (int)(i - which * n);
+            const int e = col < (int)c.whole ? col % V : V;
+            const int lane = col < (int)c.whole ? col / V : col - (int)c.whole;
+            float t = join[which][e][lane];
+            for (int k = 1; k < kTeams; ++k)
+                t += join[which][e][k * kLanes + lane];
+            out[i] = t;
         }
     }
 }

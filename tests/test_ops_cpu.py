@@ -63,7 +63,7 @@ EMB = dict(dtype=F, out=F, w=A, num=100, dim=8, ids=A, bits=64, count=4, scale=1
 @pytest.mark.parametrize("change,want", [
     (dict(dtype=3), DTYPE), (dict(dtype=H), DTYPE), (dict(dtype=H, out=B), DTYPE),
     (dict(bits=16), DTYPE), (dict(bits=0), DTYPE), (dict(num=0), SIZE),
-    (dict(num=(1 << 31) - 1), SIZE), (dict(dim=0), SIZE), (dict(dim=1 << 31), SIZE),
+    (dict(num=(1 << 31) - 1), SIZE), (dict(dim=0), SIZE), (dict(dim=(1 << 24) + 1), SIZE),
     (dict(count=-1), SIZE), (dict(count=1 << 31), SIZE), (dict(scale=NAN), ARG),
     (dict(scale=INF), ARG), (dict(w=None), NULL), (dict(ids=None), NULL), (dict(y=None), NULL),
     (dict(ids=A + 4), ALIGN), (dict(bits=32, ids=A + 2), ALIGN), (dict(w=A + 2), ALIGN),
