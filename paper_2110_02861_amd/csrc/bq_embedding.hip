@@ -43,9 +43,9 @@ __global__ __launch_bounds__(most_threads<TEAM>) void lookup_kernel(const Lookup
     constexpr int V = vec_of<WT, YT>;
     constexpr int kTeams = teams_of<TEAM>;
     using C = Cols<V, 1, TAIL>;
-    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
-    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
-    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
+    const int lanes = is_group<TEAM> ? blockDim.x : 256 / kTeams;
+    const int team = is_group<TEAM> ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = is_group<TEAM> ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const C c(a.dim, lane, lanes, (int64_t)blockIdx.y * lanes * V);
     for (int64_t t0 = ((int64_t)blockIdx.x * kTeams + team) * kLookups; t0 < a.count;
          t0 += (int64_t)gridDim.x * kTeams * kLookups) {
@@ -384,10 +384,10 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
     constexpr int kTeams = teams_of<TEAM>;
     using C = Cols<V, K, TAIL>;
     constexpr int E = C::kElems;
-    __shared__ float scratch[STABLE && TEAM == kTeamGroup ? 5 * 16 : 1];
-    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
-    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
-    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
+    __shared__ float scratch[STABLE && is_group<TEAM> ? 5 * 16 : 1];
+    const int lanes = is_group<TEAM> ? blockDim.x : 256 / kTeams;
+    const int team = is_group<TEAM> ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = is_group<TEAM> ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t dim = a.g.dim;
     const C c(dim, lane, lanes, (int64_t)blockIdx.y * lanes * K * V);
     const float rn = 1.0f / (float)dim;
@@ -431,6 +431,12 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
             for (; p < to; ++p)
                 add_rows<YT, 1>(c, s, [&](int) { return token(p); });
         };
+        const bool some = begin != end;
+        RawRow<WT, V, K, TAIL> table;
+        if constexpr (STABLE) {
+            if (TEAM == kTeam16 ? __any(some) : some)
+                load_row<WT, false>(c, row_of<WT>(a.g.table, exists ? row : 0, dim), table);
+        }
         tokens(begin, chunks ? first * kChunk : end);
         if (chunks) {
             uint32_t i = first;
@@ -451,7 +457,6 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
             if (exists)
                 store_row<WT>(c, to, s);
         } else {
-            const bool some = begin != end;
             if (TEAM == kTeam16 ? !__any(some) : !some) {
                 if (exists)
                     store_row<WT>(c, to, s);
@@ -460,7 +465,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
             // the row's statistics, as in the forward pass
             float x[E];
             float sum[1] = {0.0f};
-            load_floats<WT, V, K, TAIL>(c, row_of<WT>(a.g.table, exists ? row : 0, dim), x);
+            unpack<WT, V, K, TAIL>(table, x);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 sum[0] += x[e];
@@ -512,7 +517,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
 
 // Workgroups of the stable embedding's rows: few enough that their partial sums are
 // a small part of the work.
-constexpr int64_t kStableGroups = 512;
+constexpr int64_t kStableGroups = 1024;
 constexpr int64_t kRowGroups = 2048;  // of a plain lookup's rows
 
 struct Layout {

@@ -25,8 +25,17 @@ constexpr float kNaN = __builtin_nanf("");
 
 // ---------------------------------------------------------------------------
 // Forward.  A team takes R consecutive rows at a time, K vectors of V elements per lane
-// and row, so that R rows' loads are in flight and their sums share a barrier; it keeps
-// its columns of the parameters in registers and walks the rows with the grid.
+// and row; it keeps its columns of the parameters in registers and walks the rows with
+// the grid, the next rows' loads in flight.  HBM bounds it: 2 bytes per element each way
+// in 16 bits.
+//
+// The team for a row, measured (us, buffers larger than the memory-side cache; a wave
+// with K vectors per lane, 4 waves, or one vector per lane in as many waves as needed):
+//   32768 x 1600 bf16 (200 vectors)  wave, 4: 46   4 waves, 1: 57   2: 49
+//   32768 x 1024 bf16 (128)          wave, 2: 27   4 waves, 1: 31   2: 28
+//   16384 x 4096 bf16 (512)          wave, 8: 61   4 waves, 2: 57   4: 54   8 waves, 1: 63
+//    4096 x 8192 bf16 (1024)         4 waves, 4: 29   8: 37         16 waves, 1: 43
+// A row's own wave needs no barrier; above 4 vectors per lane its registers cost more.
 // ---------------------------------------------------------------------------
 
 template <int XT, int PT, int YT, bool GATHER, int TEAM, int K, int R, bool TAIL>
@@ -36,10 +45,10 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
     constexpr int kTeams = teams_of<TEAM>;
     using C = Cols<V, K, TAIL>;
     constexpr int E = C::kElems;
-    __shared__ float scratch[TEAM == kTeamGroup ? 3 * R * 16 : 1];
-    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
-    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
-    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
+    __shared__ float scratch[is_group<TEAM> ? 3 * R * 16 : 1];
+    const int lanes = is_group<TEAM> ? blockDim.x : 256 / kTeams;
+    const int team = is_group<TEAM> ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = is_group<TEAM> ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t n = a.cols;
     const C c(n, lane, lanes);
     const float rn = 1.0f / (float)n;
@@ -48,13 +57,12 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
         load_row<PT, false>(c, a.weight, pw);
     if (a.bias)
         load_row<PT, false>(c, a.bias, pb);
-    // (all of a workgroup's rounds are its teams' rounds, for the sums over a wave; a
-    // round's sums go to scratch behind a barrier that follows their last reading)
-    for (int64_t group = blockIdx.x; group * (kTeams * R) < a.rows; group += gridDim.x) {
+    // the next round's rows are on their way while this one's are worked on
+    RawRow<XT, V, K, TAIL> next[R];
+    bool next_known[R];
+    const auto fetch = [&](int64_t group) {
         const int64_t row0 = (group * kTeams + team) * R;
-        RawRow<XT, V, K, TAIL> raw[R];
         int64_t from[R];
-        bool known[R];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             from[j] = row0 + j < a.rows ? row0 + j : a.rows - 1;
@@ -63,12 +71,26 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
         }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            known[j] = true;
+            next_known[j] = true;
             if constexpr (GATHER) {
-                known[j] = from[j] >= 0 && from[j] < a.table_rows;
-                from[j] = known[j] ? from[j] : 0;
+                next_known[j] = from[j] >= 0 && from[j] < a.table_rows;
+                from[j] = next_known[j] ? from[j] : 0;
             }
-            load_row<XT, !GATHER>(c, row_of<XT>(a.x, from[j], a.x_stride), raw[j]);
+            load_row<XT, !GATHER>(c, row_of<XT>(a.x, from[j], a.x_stride), next[j]);
+        }
+    };
+    // (all of a workgroup's rounds are its teams' rounds, for the sums over a wave; a
+    // round's sums go to scratch behind a barrier that follows their last reading)
+    const int64_t groups = (a.rows + kTeams * R - 1) / (kTeams * R);
+    fetch(blockIdx.x);
+    for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        const int64_t row0 = (group * kTeams + team) * R;
+        RawRow<XT, V, K, TAIL> raw[R];
+        bool known[R];
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            raw[j] = next[j];
+            known[j] = next_known[j];
         }
         float x[R][E];
         float sum[R];
@@ -80,6 +102,8 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
             for (int e = 0; e < E; ++e)
                 sum[j] += x[j][e];
         }
+        if (group + gridDim.x < groups)
+            fetch(group + gridDim.x);
         team_sum<TEAM, R>(sum, scratch);
         float two[2 * R];
 #pragma unroll
@@ -210,7 +234,7 @@ void forward_k(const NormArgs &a, int threads, hipStream_t stream)
     constexpr int V = vec_of<XT, YT>;
     const int64_t rows = teams_of<TEAM> * R;
     const int64_t groups = (a.rows + rows - 1) / rows;
-    const int64_t most = 2048 * 256 / threads;
+    const int64_t most = 1024 * 256 / threads;
     const dim3 grid((unsigned)(groups < most ? groups : most)), block((unsigned)threads);
     if (a.cols % V == 0)
         hipLaunchKernelGGL((norm_forward_kernel<XT, PT, YT, GATHER, TEAM, K, R, false>), grid,
@@ -236,12 +260,16 @@ hipError_t forward(const NormArgs &a, hipStream_t stream)
         forward_k<XT, PT, YT, GATHER, kTeam16, 1, 4>(a, 256, stream);
     else if (vectors <= 64)
         forward_k<XT, PT, YT, GATHER, kTeamWave, 1, 4>(a, 256, stream);
+    else if (vectors <= 128)
+        forward_k<XT, PT, YT, GATHER, kTeamWave, 2, 2>(a, 256, stream);
+    else if (vectors <= 256)
+        forward_k<XT, PT, YT, GATHER, kTeamWave, 4, 1>(a, 256, stream);
     else if (vectors <= 512)
-        forward_k<XT, PT, YT, GATHER, kTeamGroup, 1, 4>(a, threads_of(vectors), stream);
+        forward_k<XT, PT, YT, GATHER, kTeamGroup4, 2, 1>(a, threads_of(vectors, 2), stream);
     else if (vectors <= 1024)
-        forward_k<XT, PT, YT, GATHER, kTeamGroup, 1, 2>(a, threads_of(vectors), stream);
+        forward_k<XT, PT, YT, GATHER, kTeamGroup4, 4, 1>(a, threads_of(vectors, 4), stream);
     else if (vectors <= 2048)
-        forward_k<XT, PT, YT, GATHER, kTeamGroup, 2, 1>(a, threads_of(vectors, 2), stream);
+        forward_k<XT, PT, YT, GATHER, kTeamGroup4, 8, 1>(a, threads_of(vectors, 8), stream);
     else if (vectors <= 4096)
         forward_k<XT, PT, YT, GATHER, kTeamGroup, 4, 1>(a, threads_of(vectors, 4), stream);
     else
@@ -251,12 +279,19 @@ hipError_t forward(const NormArgs &a, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Most workgroups of a backward pass of 256 threads each (four per CU).
-constexpr int64_t kNormGradGroups = 1024;
+// Most workgroups of a backward pass, of 256 threads each (fewer of larger ones).  Two per
+// CU hold enough rows in flight, and each leaves a partial row to be summed: 32768 x 1600
+// bf16 71 us at 512 and 76 at 1024, 16384 x 1024 fp32 43 and 46.
+constexpr int64_t kNormGradGroups = 512;
 
 // ---------------------------------------------------------------------------
 // Backward.  As the forward pass; each workgroup also keeps the sums of dy xh and dy of
-// its rows per column in registers and leaves them in the workspace.
+// its rows per column in registers and leaves them in the workspace.  HBM bounds it: 3
+// elements per element of the row.  The teams, measured (us, with the parameters' sums):
+//   32768 x 1600 bf16  wave, 4: 71   one vector per lane in 4 waves: 76
+//   32768 x 1024 bf16  wave, 2: 44                                   53
+//    8192 x 4096 bf16  4 waves, 2: 49   4: 57   in 8 waves: 52
+//    4096 x 8192 bf16  4 waves, 4: 50           in 16 waves: 60
 // ---------------------------------------------------------------------------
 
 template <int XT, int PT, int TEAM, int K, int R, bool TAIL>
@@ -266,10 +301,10 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_backward_kernel(const
     constexpr int kTeams = teams_of<TEAM>;
     using C = Cols<V, K, TAIL>;
     constexpr int E = C::kElems;
-    __shared__ float scratch[TEAM == kTeamGroup ? 2 * 2 * R * 16 : 1];
-    const int lanes = TEAM == kTeamGroup ? blockDim.x : 256 / kTeams;
-    const int team = TEAM == kTeamGroup ? 0 : threadIdx.x / (256 / kTeams);
-    const int lane = TEAM == kTeamGroup ? threadIdx.x : threadIdx.x % (256 / kTeams);
+    __shared__ float scratch[is_group<TEAM> ? 2 * 2 * R * 16 : 1];
+    const int lanes = is_group<TEAM> ? blockDim.x : 256 / kTeams;
+    const int team = is_group<TEAM> ? 0 : threadIdx.x / (256 / kTeams);
+    const int lane = is_group<TEAM> ? threadIdx.x : threadIdx.x % (256 / kTeams);
     const int64_t n = a.cols;
     const C c(n, lane, lanes);
     const float rn = 1.0f / (float)n;
@@ -318,7 +353,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_backward_kernel(const
         if (!a.dx)
             continue;
         team_sum<TEAM, 2 * R>(two, scratch + side);
-        if constexpr (TEAM == kTeamGroup)
+        if constexpr (is_group<TEAM>)
             side = 2 * R * 16 - side;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
@@ -434,11 +469,17 @@ int64_t backward(const NormGradArgs &a, hipStream_t stream)
         return backward_k<XT, PT, kTeam16, 1, 2>(a, 256, stream);
     if (vectors <= 64)
         return backward_k<XT, PT, kTeamWave, 1, 2>(a, 256, stream);
+    if (vectors <= 128)
+        return backward_k<XT, PT, kTeamWave, 2, 2>(a, 256, stream);
+    if (vectors <= 256)
+        return backward_k<XT, PT, kTeamWave, 4, 1>(a, 256, stream);
+    if (vectors <= 512)
+        return backward_k<XT, PT, kTeamGroup4, 2, 1>(a, threads_of(vectors, 2), stream);
     if (vectors <= 1024)
-        return backward_k<XT, PT, kTeamGroup, 1, 2>(a, threads_of(vectors), stream);
+        return backward_k<XT, PT, kTeamGroup4, 4, 1>(a, threads_of(vectors, 4), stream);
     if (vectors <= 2048)
         return backward_k<XT, PT, kTeamGroup, 2, 1>(a, threads_of(vectors, 2), stream);
-    const int64_t groups = a.rows < 512 ? a.rows : 512;
+    const int64_t groups = a.rows < kNormGradGroups ? a.rows : kNormGradGroups;
     hipLaunchKernelGGL((norm_backward_long_kernel<XT, PT>), dim3((unsigned)groups),
                        dim3(64 * kLongWaves), 0, stream, a);
     return groups;
@@ -459,7 +500,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void param_grads_kernel(const float
     const int which = blockIdx.y;
     float s = 0.0f;
     if (c < cols) {
-#pragma unroll 4
+#pragma unroll 16
         for (int64_t g = wave; g < groups; g += kSumWaves)
             s += G(partials)[(2 * g + which) * cols + c];
     }

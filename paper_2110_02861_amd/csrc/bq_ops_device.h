@@ -205,10 +205,13 @@ __device__ inline float wave_sum(float v)
 }
 
 // A team of lanes holds a row: 16 lanes (four teams to a wave), a wave (four to a
-// workgroup), or a workgroup of as many waves as the row needs.
-enum { kTeam16 = 0, kTeamWave = 1, kTeamGroup = 2 };
+// workgroup), or a workgroup of as many waves as the row needs, up to 4 or up to 16 (of
+// which each has half as many registers).
+enum { kTeam16 = 0, kTeamWave = 1, kTeamGroup4 = 2, kTeamGroup = 3 };
 template <int TEAM>
 constexpr int teams_of = TEAM == kTeam16 ? 16 : TEAM == kTeamWave ? 4 : 1;
+template <int TEAM>
+constexpr bool is_group = TEAM == kTeamGroup4 || TEAM == kTeamGroup;
 template <int TEAM>
 constexpr int most_threads = TEAM == kTeamGroup ? 1024 : 256;
 
@@ -229,7 +232,7 @@ __device__ inline void team_sum(float (&v)[N], float *scratch)
             v[i] = wave_sum(v[i]);
         }
     }
-    if constexpr (TEAM == kTeamGroup) {
+    if constexpr (is_group<TEAM>) {
         const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
@@ -346,35 +349,53 @@ __device__ inline void store_row(const Cols<V, K, TAIL> &c, void *row,
 }
 
 // Leaves a workgroup's sums per column of two gradients in out[2][n]: its only team's, or
-// (K == 1) its teams' in order.  All threads call it.
+// its teams' in order, a vector per lane at a time.  All threads call it.
 template <int TEAM, int V, int K, bool TAIL>
 __device__ inline void leave_partials(const Cols<V, K, TAIL> &c,
                                       const float (&dw)[K * V + (TAIL ? 1 : 0)],
                                       const float (&db)[K * V + (TAIL ? 1 : 0)], int64_t n,
                                       float *out)
 {
-    if constexpr (TEAM == kTeamGroup) {
+    if constexpr (is_group<TEAM>) {
         store_row<kF32>(c, out, dw);
         store_row<kF32>(c, out + n, db);
     } else {
         constexpr int kTeams = teams_of<TEAM>, kLanes = 256 / kTeams;
-        static_assert(K == 1, "a team of a wave or less holds one vector per lane");
-        constexpr int E = V + (TAIL ? 1 : 0);
-        __shared__ float join[2][E][256];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            join[0][e][threadIdx.x] = dw[e];
-            join[1][e][threadIdx.x] = db[e];
-        }
-        __syncthreads();
-        for (int64_t i = threadIdx.x; i < 2 * n; i += 256) {
-            const int which = i >= n, col = (int)(i - which * n);
-            const int e = col < (int)c.whole ? col % V : V;
-            const int lane = col < (int)c.whole ? col / V : col - (int)c.whole;
-            float t = join[which][e][lane];
+        __shared__ float join[2][V][256];
+        const auto add = [&](int which, int r, int lane) {
+            float t = join[which][r][lane];
             for (int k = 1; k < kTeams; ++k)
-                t += join[which][e][k * kLanes + lane];
-            out[i] = t;
+                t += join[which][r][k * kLanes + lane];
+            return t;
+        };
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < V; ++r) {
+                join[0][r][threadIdx.x] = dw[k * V + r];
+                join[1][r][threadIdx.x] = db[k * V + r];
+            }
+            __syncthreads();
+            const uint32_t first = k * c.stride;
+            const uint32_t cols = first >= c.whole ? 0 : min(c.stride, c.whole - first);
+            for (uint32_t i = threadIdx.x; i < 2 * cols; i += 256) {
+                const int which = i >= cols;
+                const uint32_t col = i - which * cols;
+                out[which * n + first + col] = add(which, col % V, col / V);
+            }
+        }
+        if constexpr (TAIL) {
+            __syncthreads();
+            join[0][0][threadIdx.x] = dw[K * V];
+            join[1][0][threadIdx.x] = db[K * V];
+            __syncthreads();
+            const uint32_t cols = (uint32_t)n - c.whole;
+            if (threadIdx.x < 2 * cols) {
+                const int which = threadIdx.x >= cols;
+                const uint32_t col = threadIdx.x - which * cols;
+                out[which * n + c.whole + col] = add(which, 0, col);
+            }
         }
     }
 }
