@@ -30,6 +30,22 @@ __device__ inline int tensor_of(const ClipArgs &a, int tile, int from)
     return lo;
 }
 
+// The same where it is `from` or one before it.
+__device__ inline int tensor_below(const ClipArgs &a, int tile, int from)
+{
+    if (a.tile_begin[from] <= tile)
+        return from;
+    int lo = 0, hi = from - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.tile_begin[mid] <= tile)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    return lo;
+}
+
 __device__ inline double wave_add(double v)
 {
 #pragma unroll
@@ -46,28 +62,74 @@ __device__ inline uint32_t wave_umax(uint32_t v)
     return v;
 }
 
+constexpr int kVecs = kClipTileBytes / 16 / kThreads;  // of 16 bytes, per thread and tile
+
+// A tile's values as they are in memory: 16 bytes at a time, zeros behind the tensor's
+// end.  (A last vector's elements are loaded one by one, by one lane.)
+struct Tile {
+    vu4 w[kVecs];
+    int dtype;
+};
 template <int DT>
-__device__ inline void tile_norm(const void *p, int64_t from, int64_t numel, bool inf_norm,
-                                 double (&acc)[2], uint32_t &top)
+__device__ inline vu4 load16(const void *p, int64_t e, int64_t numel)
 {
-    constexpr int V = DT == kF32 ? 4 : 8;
-    constexpr int kVecs = kClipTileBytes / 16 / kThreads;
-    float x[kVecs][V];
+    constexpr int V = 16 / elem_bytes<DT>;
+    vu4 w = {0, 0, 0, 0};
+    if (e + V <= numel) {
+        const Raw<DT, V> x = load_raw<DT, V, true>(p, e);
+        w = vu4{x.w[0], x.w[1], x.w[2], x.w[3]};
+    } else if (e < numel) {
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-        load_cols<DT, V>(p, from + (int64_t)(k * kThreads + threadIdx.x) * V, numel, x[k]);
-    if (inf_norm) {
+        for (int r = 0; r < V; ++r) {
+            if (e + r < numel) {
+                if constexpr (DT == kF32)
+                    w[r] = G(static_cast<const uint32_t *>(p))[e + r];
+                else
+                    w[r / 2] |= (uint32_t)G(static_cast<const uint16_t *>(p))[e + r] << (16 * (r % 2));
+            }
+        }
+    }
+    return w;
+}
+__device__ inline void load_tile(const ClipArgs &a, int t, int tile, Tile &x)
+{
+    const void *const p = a.ptr[t];
+    const int64_t n = a.numel[t];
+    x.dtype = a.dtype[t];
+    const int elems = x.dtype == kF32 ? 4 : 8;  // per vector
+    const int64_t from = (int64_t)(tile - a.tile_begin[t]) * (kClipTileBytes / 16) * elems;
+    if (from + kClipTileBytes / 16 * elems <= n) {
+        const char *const q = static_cast<const char *>(p) + from / elems * 16;
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k)
+        for (int k = 0; k < kVecs; ++k) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(q) + (k * kThreads + threadIdx.x) * 16;
+            x.w[k] = __builtin_nontemporal_load((gvu4_any2)at);
+        }
+        return;
+    }
 #pragma unroll
-            for (int r = 0; r < V; ++r)
-                top = max(top, __float_as_uint(x[k][r]) & 0x7fffffffu);
-    } else {
+    for (int k = 0; k < kVecs; ++k) {
+        const int64_t e = from + (int64_t)(k * kThreads + threadIdx.x) * elems;
+        x.w[k] = x.dtype == kF32 ? load16<kF32>(p, e, n) : load16<kF16>(p, e, n);
+    }
+}
+
+template <int DT>
+__device__ inline void add_tile(const Tile &x, bool inf_norm, double (&acc)[2], uint32_t &top)
+{
+    constexpr int V = 16 / elem_bytes<DT>;
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k)
+    for (int k = 0; k < kVecs; ++k) {
+        const Raw<DT, V> raw = {x.w[k].x, x.w[k].y, x.w[k].z, x.w[k].w};
+        float f[V];
+        unpack<DT, V>(raw, f);
 #pragma unroll
-            for (int r = 0; r < V; ++r)
-                acc[r & 1] = __builtin_fma((double)x[k][r], (double)x[k][r], acc[r & 1]);
+        for (int r = 0; r < V; ++r) {
+            if (inf_norm)
+                top = max(top, __float_as_uint(f[r]) & 0x7fffffffu);
+            else
+                acc[r & 1] = __builtin_fma((double)f[r], (double)f[r], acc[r & 1]);
+        }
     }
 }
 
@@ -77,17 +139,22 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const ClipArgs a)
     __shared__ uint32_t tops[kThreads / 64];
     double acc[2] = {0.0, 0.0};
     uint32_t top = 0;
-    int t = 0;
+    // the next tile's values are on their way while this one's are added
+    Tile next;
+    int t = tensor_of(a, blockIdx.x, 0);
+    load_tile(a, t, blockIdx.x, next);
     for (int tile = blockIdx.x; tile < a.total_tiles; tile += gridDim.x) {
-        t = tensor_of(a, tile, t);
-        const void *const p = a.ptr[t];
-        const int64_t at = tile - a.tile_begin[t], n = a.numel[t];
-        if (a.dtype[t] == kF32)
-            tile_norm<kF32>(p, at * (kClipTileBytes / 4), n, a.inf_norm, acc, top);
-        else if (a.dtype[t] == kF16)
-            tile_norm<kF16>(p, at * (kClipTileBytes / 2), n, a.inf_norm, acc, top);
+        const Tile x = next;
+        if (tile + (int)gridDim.x < a.total_tiles) {
+            t = tensor_of(a, tile + gridDim.x, t);
+            load_tile(a, t, tile + gridDim.x, next);
+        }
+        if (x.dtype == kF32)
+            add_tile<kF32>(x, a.inf_norm, acc, top);
+        else if (x.dtype == kF16)
+            add_tile<kF16>(x, a.inf_norm, acc, top);
         else
-            tile_norm<kBF16>(p, at * (kClipTileBytes / 2), n, a.inf_norm, acc, top);
+            add_tile<kBF16>(x, a.inf_norm, acc, top);
     }
     const double s = wave_add(acc[0] + acc[1]);
     top = wave_umax(top);
@@ -149,20 +216,21 @@ __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double *par
 }
 
 template <int DT>
-__device__ inline void tile_scale(void *p, int64_t from, int64_t numel, float c)
+__device__ inline void scale_tile(const ClipArgs &a, int t, int tile, const Tile &x, float c)
 {
-    constexpr int V = DT == kF32 ? 4 : 8;
-    constexpr int kVecs = kClipTileBytes / 16 / kThreads;
-    float x[kVecs][V];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-        load_cols<DT, V>(p, from + (int64_t)(k * kThreads + threadIdx.x) * V, numel, x[k]);
+    constexpr int V = 16 / elem_bytes<DT>;
+    void *const p = a.ptr[t];
+    const int64_t n = a.numel[t];
+    const int64_t from = (int64_t)(tile - a.tile_begin[t]) * (kClipTileBytes / 16) * V;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
+        const Raw<DT, V> raw = {x.w[k].x, x.w[k].y, x.w[k].z, x.w[k].w};
+        float f[V];
+        unpack<DT, V>(raw, f);
 #pragma unroll
         for (int r = 0; r < V; ++r)
-            x[k][r] *= c;
-        store_cols<DT, V>(p, from + (int64_t)(k * kThreads + threadIdx.x) * V, numel, x[k]);
+            f[r] *= c;
+        store_cols<DT, V>(p, from + (int64_t)(k * kThreads + threadIdx.x) * V, n, f);
     }
 }
 
@@ -176,17 +244,20 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const ClipArgs a)
     const float c = (float)(ratio > 1.0 ? 1.0 : ratio);  // NaN stays
     if (c == 1.0f)
         return;
-    int t = 0;
-    for (int tile = blockIdx.x; tile < a.total_tiles; tile += gridDim.x) {
-        t = tensor_of(a, tile, t);
-        void *const p = a.ptr[t];
-        const int64_t at = tile - a.tile_begin[t], n = a.numel[t];
-        if (a.dtype[t] == kF32)
-            tile_scale<kF32>(p, at * (kClipTileBytes / 4), n, c);
-        else if (a.dtype[t] == kF16)
-            tile_scale<kF16>(p, at * (kClipTileBytes / 2), n, c);
+    // from the last tile down: the norm launches read it last, and some of it may still be
+    // in the memory-side cache
+    int last = a.ntensors - 1;
+    for (int i = blockIdx.x; i < a.total_tiles; i += gridDim.x) {
+        const int tile = a.total_tiles - 1 - i;
+        last = tensor_below(a, tile, last);
+        Tile x;
+        load_tile(a, last, tile, x);
+        if (x.dtype == kF32)
+            scale_tile<kF32>(a, last, tile, x, c);
+        else if (x.dtype == kF16)
+            scale_tile<kF16>(a, last, tile, x, c);
         else
-            tile_scale<kBF16>(p, at * (kClipTileBytes / 2), n, c);
+            scale_tile<kBF16>(a, last, tile, x, c);
     }
 }
 
@@ -207,7 +278,7 @@ hipError_t launch_norm_finish(const ClipArgs &a, double *total, hipStream_t stre
 
 hipError_t launch_clip(const ClipArgs &a, hipStream_t stream)
 {
-    const int groups = a.total_tiles < 2048 ? (a.total_tiles < 1 ? 1 : a.total_tiles) : 2048;
+    const int groups = a.total_tiles < 4096 ? a.total_tiles : 4096;
     hipLaunchKernelGGL(clip_kernel, dim3((unsigned)groups), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }

@@ -77,8 +77,9 @@ __global__ __launch_bounds__(most_threads<TEAM>) void lookup_kernel(const Lookup
 // ---------------------------------------------------------------------------
 // Sort of (id, position) pairs by id: radix passes from the low digit up, each
 // stable.  At most kSortTiles tiles of the list, one workgroup each; the counts of
-// the digits in every tile give each tile its places, and a pass counts the next
-// digit as it places the pairs.
+// the digits in every tile give each tile its places.  (Counting the next pass's digits
+// in global memory while pairs are placed saves a launch and loses 8 us by it: the same
+// few counters take most of the additions.)
 // ---------------------------------------------------------------------------
 
 constexpr int kSortThreads = 512;
@@ -87,6 +88,7 @@ constexpr int kSortItems = 2;                             // per thread and subt
 constexpr int kSubtile = kSortThreads * kSortItems;       // 1024
 constexpr int kSortTiles = 128;
 constexpr int kMaxBins = 1024;
+constexpr int kSmallSort = 4096;  // tokens that one workgroup sorts by itself
 
 struct SortShape {
     int bits, passes;   // per pass; bins = 1 << bits
@@ -98,7 +100,8 @@ SortShape sort_shape(int64_t count, int64_t num)
     int bits = 1;
     while ((num >> bits) != 0)  // keys 0 .. num
         ++bits;
-    s.passes = bits <= 8 ? 1 : bits <= 20 ? 2 : bits <= 30 ? 3 : 4;
+    s.passes = count <= kSmallSort ? (bits + 7) / 8  // of at most kSmallBins digits
+               : bits <= 8 ? 1 : bits <= 20 ? 2 : bits <= 30 ? 3 : 4;
     s.bits = (bits + s.passes - 1) / s.passes;
     s.tile = kSubtile;
     while (s.tile * kSortTiles < count)
@@ -111,9 +114,9 @@ struct SortArgs {
     const void *ids;     // the first pass reads these
     const uint2 *in;     // the others these: {key, position}
     uint2 *out;
-    uint32_t *hist;      // passes x tiles x bins
+    uint32_t *hist;      // tiles x bins, of the pass
     int64_t count, num, tile, tiles;
-    int32_t ids64, bits, pass, passes, tile_log2;
+    int32_t ids64, bits, pass, passes;
 };
 
 // Id as a key: ids outside of the table get the key behind its rows.
@@ -123,22 +126,115 @@ __device__ inline uint32_t key_at(const SortArgs &a, int64_t i)
     return id >= 0 && id < a.num ? (uint32_t)id : (uint32_t)a.num;
 }
 
+// The pass's digit of the pairs in every tile.
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a)
 {
     __shared__ uint32_t bins[kMaxBins];
-    const int n = 1 << a.bits;
+    const int n = 1 << a.bits, shift = a.bits * a.pass;
     for (int i = threadIdx.x; i < n; i += kSortThreads)
         bins[i] = 0;
     __syncthreads();
     const int64_t begin = blockIdx.x * a.tile;
     const int64_t end = begin + a.tile < a.count ? begin + a.tile : a.count;
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads)
-        atomicAdd(&bins[key_at(a, i) & (n - 1)], 1u);
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
+        const uint32_t key = a.pass == 0 ? key_at(a, i) : a.in[i].x;
+        atomicAdd(&bins[(key >> shift) & (n - 1)], 1u);
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kSortThreads) {
+    for (int i = threadIdx.x; i < n; i += kSortThreads)
         a.hist[(int64_t)blockIdx.x * n + i] = bins[i];
-        for (int p = 1; p < a.passes; ++p)  // later passes count into these
-            a.hist[((int64_t)p * a.tiles + blockIdx.x) * n + i] = 0;
+}
+
+// Rank of a pair among the wave's earlier pairs with its digit d, which `count` holds
+// for the wave's earlier rounds and then for this one too.
+__device__ inline uint32_t wave_rank(uint32_t d, bool live, int bits, uint32_t *count)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t same = __ballot(live);  // the lanes with the same digit
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((d >> b) & 1u);
+        same &= (d >> b) & 1u ? set : ~set;
+    }
+    const int leader = same ? __ffsll((unsigned long long)same) - 1 : 0;
+    uint32_t old = 0;
+    if (live && lane == leader)
+        old = atomicAdd(&count[d], (uint32_t)__popcll(same));
+    old = __shfl(old, leader);
+    return old + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+}
+
+// Few tokens: one workgroup, which keeps the pairs on chip from pass to pass.
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallItems = 4;
+static_assert(kSmallSort == kSmallThreads * kSmallItems, "a pair per thread and item");
+constexpr int kSmallBins = 256;
+__global__ __launch_bounds__(kSmallThreads) void sort_small_kernel(const SortArgs a)
+{
+    __shared__ uint2 pairs[kSmallSort];
+    __shared__ uint32_t count[kSmallWaves][kSmallBins];
+    __shared__ uint32_t sums[kSmallWaves];
+    const int n = 1 << a.bits;
+    const uint32_t mask = (uint32_t)n - 1;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    uint2 pair[kSmallItems];
+    bool live[kSmallItems];
+#pragma unroll
+    for (int k = 0; k < kSmallItems; ++k) {
+        const int i = wave * (64 * kSmallItems) + k * 64 + lane;
+        live[k] = i < a.count;
+        pair[k] = uint2{live[k] ? key_at(a, i) : 0u, (uint32_t)i};
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = a.bits * pass;
+        for (int i = threadIdx.x; i < kSmallWaves * kSmallBins; i += kSmallThreads)
+            (&count[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t rank[kSmallItems];
+#pragma unroll
+        for (int k = 0; k < kSmallItems; ++k)
+            rank[k] = wave_rank((pair[k].x >> shift) & mask, live[k], a.bits, count[wave]);
+        __syncthreads();
+        // where each wave's pairs of a digit start
+        uint32_t total = 0;
+        if (threadIdx.x < kSmallBins) {
+#pragma unroll
+            for (int w = 0; w < kSmallWaves; ++w)
+                total += count[w][threadIdx.x];
+        }
+        const uint32_t incl = wave_scan(total);
+        if (lane == 63)
+            sums[wave] = incl;
+        __syncthreads();
+        if (threadIdx.x < kSmallBins) {
+            uint32_t at = incl - total;
+            for (int w = 0; w < wave; ++w)
+                at += sums[w];
+#pragma unroll
+            for (int w = 0; w < kSmallWaves; ++w) {
+                const uint32_t c = count[w][threadIdx.x];
+                count[w][threadIdx.x] = at;
+                at += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSmallItems; ++k) {
+            const uint32_t at = count[wave][(pair[k].x >> shift) & mask] + rank[k];
+            if (live[k]) {
+                if (pass + 1 == a.passes)
+                    a.out[at] = pair[k];
+                else
+                    pairs[at] = pair[k];
+            }
+        }
+        if (pass + 1 == a.passes)
+            return;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSmallItems; ++k)
+            if (live[k])
+                pair[k] = pairs[wave * (64 * kSmallItems) + k * 64 + lane];
     }
 }
 
@@ -152,7 +248,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int shift = a.bits * a.pass;
     const uint32_t mask = (uint32_t)n - 1;
-    const uint32_t *const hist = a.hist + (int64_t)a.pass * a.tiles * n;
+    const uint32_t *const hist = a.hist;
 
     // the digits' counts in all tiles, and in the tiles before this one: where there
     // are fewer digits than threads, the threads of a digit share the tiles
@@ -197,8 +293,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
 
     const int64_t begin = blockIdx.x * a.tile;
     const int64_t end = begin + a.tile < a.count ? begin + a.tile : a.count;
-    const bool last = a.pass + 1 == a.passes;
-    uint32_t *const next = a.hist + (int64_t)(a.pass + 1) * a.tiles * n;
     for (int64_t sub = begin; sub < end; sub += kSubtile) {
         __syncthreads();  // place is up to date, count has been read
         for (int i = threadIdx.x; i < kSortWaves * n; i += kSortThreads)
@@ -225,21 +319,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
             }
         }
 #pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const uint32_t d = (key[k] >> shift) & mask;
-            // the lanes with the same digit
-            uint64_t same = __ballot(live[k]);
-            for (int b = 0; b < a.bits; ++b) {
-                const uint64_t set = __ballot((d >> b) & 1u);
-                same &= (d >> b) & 1u ? set : ~set;
-            }
-            const int leader = same ? __ffsll((unsigned long long)same) - 1 : 0;
-            uint32_t old = 0;
-            if (live[k] && lane == leader)
-                old = atomicAdd(&count[wave][d], (uint32_t)__popcll(same));
-            old = __shfl(old, leader);
-            rank[k] = old + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        }
+        for (int k = 0; k < kSortItems; ++k)
+            rank[k] = wave_rank((key[k] >> shift) & mask, live[k], a.bits, count[wave]);
         __syncthreads();
         // where each wave's pairs of a digit start
         for (int d = threadIdx.x; d < n; d += kSortThreads) {
@@ -258,9 +339,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
             if (live[k]) {
                 const uint32_t at = count[wave][(key[k] >> shift) & mask] + rank[k];
                 a.out[at] = uint2{key[k], pos[k]};
-                if (!last)
-                    atomicAdd(&next[(int64_t)(at >> a.tile_log2) * n + ((key[k] >> (shift + a.bits)) & mask)],
-                              1u);
             }
         }
     }
@@ -274,7 +352,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
 constexpr int kChunk = 32;
 constexpr int kBatch = 8;  // rows in flight per thread
 
+// What an earlier launch wrote, read by scalar loads where a wave's lanes agree.
 typedef const __attribute__((address_space(4))) uint32_t *cptr;
+__device__ inline int64_t uniform(int64_t v)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)v) |
+                     (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32);
+}
 
 struct GradArgs {
     LookupGradArgs g;
@@ -396,21 +480,30 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
     for (int e = 0; e < E; ++e)
         dw[e] = db[e] = 0.0f;
 
+    // where a row's tokens are, asked for a round ahead
+    const auto places = [&](int64_t row, uint32_t &begin, uint32_t &end) {
+        begin = end = 0;
+        if (row < a.g.num && (STABLE || row != a.g.padding)) {
+            if constexpr (TEAM == kTeam16) {
+                begin = a.starts[row];
+                end = a.starts[row + 1];
+            } else {
+                const int64_t at = uniform(row);
+                begin = ((cptr)a.starts)[at];
+                end = ((cptr)a.starts)[at + 1];
+            }
+        }
+    };
+    uint32_t next_begin, next_end;
+    places((int64_t)blockIdx.x * kTeams + team, next_begin, next_end);
     // (a workgroup's teams leave together, for the sums over the wave)
     for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < a.g.num;
          row0 += (int64_t)gridDim.x * kTeams) {
         const int64_t row = row0 + team;
         const bool exists = row < a.g.num;
         const bool padding = row == a.g.padding;
-        uint32_t begin = 0, end = 0;
-        if (exists && (STABLE || !padding)) {
-            begin = a.starts[row];
-            end = a.starts[row + 1];
-        }
-        if constexpr (TEAM != kTeam16) {
-            begin = __builtin_amdgcn_readfirstlane(begin);
-            end = __builtin_amdgcn_readfirstlane(end);
-        }
+        const uint32_t begin = next_begin, end = next_end;
+        places(row + (int64_t)gridDim.x * kTeams, next_begin, next_end);
         float s[E];
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -419,8 +512,6 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
         const uint32_t first = (begin + kChunk - 1) / kChunk, last = end / kChunk;
         const bool chunks = first < last;
         const auto token = [&](uint32_t p) {
-            // (the sorted list was written by an earlier launch: scalar loads where p is
-            // the same for the wave)
             const uint32_t at = TEAM == kTeam16 ? a.sorted[p].y
                                                 : ((cptr)a.sorted)[2 * (uint64_t)p + 1];
             return row_of<YT>(a.g.dout, at, dim);
@@ -530,7 +621,7 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     l.pairs_a = 0;
     l.pairs_b = l.pairs_a + round_up(count * 8, 256);
     l.hist = l.pairs_b + (s.passes > 1 ? round_up(count * 8, 256) : 0);
-    l.starts = l.hist + round_up((int64_t)s.passes * s.tiles * 4 << s.bits, 256);
+    l.starts = l.hist + round_up(s.tiles * 4 << s.bits, 256);
     l.chunks = l.starts + round_up((num + 1) * 4, 256);
     l.partials = l.chunks + round_up(count / kChunk * dim * 4, 256);
     l.bytes = l.partials + (stable ? kStableGroups * 2 * dim * 4 : 0);
@@ -646,15 +737,19 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
         s.tiles = shape.tiles;
         s.ids64 = g.ids64;
         s.bits = shape.bits;
-        s.tile_log2 = 63 - __builtin_clzll((unsigned long long)shape.tile);
         s.passes = shape.passes;
         s.pass = 0;
         const dim3 grid((unsigned)shape.tiles), block(kSortThreads);
-        hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, stream, s);
-        for (; s.pass < s.passes; ++s.pass) {
-            s.out = s.pass % 2 ? pb : pa;
-            hipLaunchKernelGGL(sort_place_kernel, grid, block, 0, stream, s);
+        if (g.count <= kSmallSort) {
+            hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSmallThreads), 0, stream, s);
             s.in = s.out;
+        } else {
+            for (; s.pass < s.passes; ++s.pass) {
+                s.out = s.pass % 2 ? pb : pa;
+                hipLaunchKernelGGL(sort_count_kernel, grid, block, 0, stream, s);
+                hipLaunchKernelGGL(sort_place_kernel, grid, block, 0, stream, s);
+                s.in = s.out;
+            }
         }
         a.sorted = s.in;
     }

@@ -357,6 +357,20 @@ int32_t pack(const bq_grad *grads, int32_t ngrads, int32_t at, bq::ClipArgs &a)
     return at;
 }
 
+// As pack, with the last non-empty gradients before `at`; returns the first's index.
+int32_t pack_below(const bq_grad *grads, int32_t at, bq::ClipArgs &a)
+{
+    int32_t from = at;
+    for (int32_t n = 0; from > 0; --from) {
+        if (grads[from - 1].numel == 0)
+            continue;
+        if (n++ == bq::kMaxClipTensors)
+            break;
+    }
+    pack(grads, at, from, a);
+    return from;
+}
+
 bq_status norm_and_clip(const bq_grad *grads, int32_t ngrads, bq_norm kind, bool clip,
                         double max_norm, void *workspace, float *norm, hipStream_t stream)
 {
@@ -386,8 +400,9 @@ bq_status norm_and_clip(const bq_grad *grads, int32_t ngrads, bq_norm kind, bool
         a.npartials = 1;
         a.norm = nullptr;
     }
-    for (int32_t at = 0; at < ngrads;) {
-        at = pack(grads, ngrads, at, a);
+    // the launches in the opposite order: what the norm read last comes first
+    for (int32_t at = ngrads; at > 0;) {
+        at = pack_below(grads, at, a);
         if (a.ntensors == 0)
             break;
         const hipError_t e = bq::launch_clip(a, stream);
