@@ -31,45 +31,64 @@ constexpr int vec_of = (elem_bytes<A> == 4 || elem_bytes<B> == 4) ? 4 : 8;
 constexpr float kNaN = __builtin_nanf("");
 
 // ---------------------------------------------------------------------------
-// Lookup.  A team takes four tokens at a time, whose rows' loads are in flight together;
-// longer rows are cut into slabs (blockIdx.y).
+// Lookup.  A wave holds R tokens' rows, K vectors per lane (16 lanes hold short ones;
+// longer rows are cut into slabs, blockIdx.y).  The table's rows come from the caches
+// where tokens repeat, so reading them counts as much as writing the result: 65536
+// tokens, 1600 fp32 to bf16 86 us (420 MB looked up, 210 written), 32768 to fp32 51 us;
+// with rows held by workgroups of 7 waves 98 and 67, 4 vectors per lane and 2 slabs 86
+// and 71.
 // ---------------------------------------------------------------------------
 
-constexpr int kLookups = 4;
-
-template <int WT, int YT, int TEAM, bool TAIL>
-__global__ __launch_bounds__(most_threads<TEAM>) void lookup_kernel(const LookupArgs a)
+template <int WT, int YT, int TEAM, int K, int R, bool TAIL>
+__global__ __launch_bounds__(256) void lookup_kernel(const LookupArgs a)
 {
     constexpr int V = vec_of<WT, YT>;
     constexpr int kTeams = teams_of<TEAM>;
-    using C = Cols<V, 1, TAIL>;
-    const int lanes = is_group<TEAM> ? blockDim.x : 256 / kTeams;
-    const int team = is_group<TEAM> ? 0 : threadIdx.x / (256 / kTeams);
-    const int lane = is_group<TEAM> ? threadIdx.x : threadIdx.x % (256 / kTeams);
-    const C c(a.dim, lane, lanes, (int64_t)blockIdx.y * lanes * V);
-    for (int64_t t0 = ((int64_t)blockIdx.x * kTeams + team) * kLookups; t0 < a.count;
-         t0 += (int64_t)gridDim.x * kTeams * kLookups) {
-        int64_t id[kLookups];
-        RawRow<WT, V, 1, TAIL> raw[kLookups];
+    using C = Cols<V, K, TAIL>;
+    const int lanes = 256 / kTeams, team = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+    const C c(a.dim, lane, lanes, (int64_t)blockIdx.y * lanes * K * V);
+    const int64_t step = (int64_t)gridDim.x * kTeams * R;
+    const bool streams = stream_lookup(a.count * a.dim * elem_bytes<YT>);
+    // the next tokens' rows are on their way while this round's are stored
+    RawRow<WT, V, K, TAIL> next[R];
+    bool next_known[R];
+    const auto fetch = [&](int64_t t0) {
+        int64_t id[R];
 #pragma unroll
-        for (int j = 0; j < kLookups; ++j)
+        for (int j = 0; j < R; ++j)
             id[j] = id_at(a.ids, t0 + j < a.count ? t0 + j : a.count - 1, a.ids64);
 #pragma unroll
-        for (int j = 0; j < kLookups; ++j) {
-            const bool known = id[j] >= 0 && id[j] < a.num;
-            load_row<WT, false>(c, row_of<WT>(a.table, known ? id[j] : 0, a.dim), raw[j]);
+        for (int j = 0; j < R; ++j) {
+            next_known[j] = id[j] >= 0 && id[j] < a.num;
+            load_row<WT, false>(c, row_of<WT>(a.table, next_known[j] ? id[j] : 0, a.dim), next[j]);
         }
+    };
+    int64_t t0 = ((int64_t)blockIdx.x * kTeams + team) * R;
+    if (t0 < a.count)
+        fetch(t0);
+    for (; t0 < a.count; t0 += step) {
+        RawRow<WT, V, K, TAIL> raw[R];
+        bool known[R];
 #pragma unroll
-        for (int j = 0; j < kLookups; ++j) {
+        for (int j = 0; j < R; ++j) {
+            raw[j] = next[j];
+            known[j] = next_known[j];
+        }
+        if (t0 + step < a.count)
+            fetch(t0 + step);
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
             if (t0 + j >= a.count)
                 break;
-            const bool known = id[j] >= 0 && id[j] < a.num;
             float x[C::kElems];
-            unpack<WT, V, 1, TAIL>(raw[j], x);
+            unpack<WT, V, K, TAIL>(raw[j], x);
 #pragma unroll
             for (int e = 0; e < C::kElems; ++e)
-                x[e] = known ? x[e] * a.scale : kNaN;
-            store_row<YT>(c, row_of<YT>(a.out, t0 + j, a.dim), x);
+                x[e] = known[j] ? x[e] * a.scale : kNaN;
+            if (streams)
+                store_row<YT, true>(c, row_of<YT>(a.out, t0 + j, a.dim), x);
+            else
+                store_row<YT>(c, row_of<YT>(a.out, t0 + j, a.dim), x);
         }
     }
 }
@@ -606,10 +625,14 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
     }
 }
 
-// Workgroups of the stable embedding's rows: few enough that their partial sums are
-// a small part of the work.
-constexpr int64_t kStableGroups = 1024;
-constexpr int64_t kRowGroups = 2048;  // of a plain lookup's rows
+// Workgroups of a plain lookup's rows, at most.  Walking the table evens out rows of
+// many tokens; the whole backward pass, 50257 rows of 1600 fp32, 65536 tokens: 178 us at
+// 1024, 158 at 2048, 151 at 4096 and at 8192, 176 with one for every row.
+constexpr int64_t kRowGroups = 8192;
+// Of the stable embedding's, of which each also leaves a partial row: the same 258 us at
+// 512, 224 at 768, 212 at 1024, 224 at 1280; short rows, whose workgroups are smaller, take
+// twice as many.
+constexpr int64_t stable_groups(int64_t dim) { return dim <= 1024 ? 2048 : 1024; }
 
 struct Layout {
     int64_t pairs_a, pairs_b, hist, starts, chunks, partials, bytes;
@@ -624,7 +647,7 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     l.starts = l.hist + round_up(s.tiles * 4 << s.bits, 256);
     l.chunks = l.starts + round_up((num + 1) * 4, 256);
     l.partials = l.chunks + round_up(count / kChunk * dim * 4, 256);
-    l.bytes = l.partials + (stable ? kStableGroups * 2 * dim * 4 : 0);
+    l.bytes = l.partials + (stable ? stable_groups(dim) * 2 * dim * 4 : 0);
     return l;
 }
 
@@ -642,7 +665,7 @@ int64_t rows_k(const GradArgs &a, int threads, hipStream_t stream)
 {
     constexpr int V = vec_of<WT, YT>;
     constexpr int kTeams = teams_of<TEAM>;
-    const int64_t most = STABLE ? kStableGroups : kRowGroups;
+    const int64_t most = STABLE ? stable_groups(a.g.dim) : kRowGroups;
     int64_t groups = (a.g.num + kTeams - 1) / kTeams;
     groups = groups < most ? groups : most;
     const dim3 grid((unsigned)groups, slabs_of<V>(a.g.dim, (int64_t)threads / kTeams * K * V));
@@ -661,7 +684,11 @@ int threads_of(int64_t vectors, int k = 1)
     return (int)((vectors + 64 * k - 1) / (64 * k) * 64);
 }
 
-// The team that holds a row, and the launch; returns the workgroups.
+// The team that holds a row, and the launch; returns the workgroups.  The stable
+// embedding's rows want few waves at a barrier, the plain sums many loads in flight for
+// the same tokens: backward passes of 65536 tokens, 50257 rows of 1600 fp32 (400 vectors),
+// in us:  one vector per lane, 7 waves: plain 151, stable 257;  4 waves, 2: 166, 212;
+// 2 waves, 4: 192, 230;  a wave, 8: 235, 266.
 template <int WT, int YT, bool STABLE>
 int64_t rows(const GradArgs &a, hipStream_t stream)
 {
@@ -671,29 +698,37 @@ int64_t rows(const GradArgs &a, hipStream_t stream)
         return rows_k<WT, YT, kTeam16, 1, STABLE>(a, 256, stream);
     if (vectors <= 64)
         return rows_k<WT, YT, kTeamWave, 1, STABLE>(a, 256, stream);
-    if (vectors <= 1024)
-        return rows_k<WT, YT, kTeamGroup, 1, STABLE>(a, threads_of(vectors), stream);
-    if constexpr (STABLE && V == 4) {
-        if (vectors > 2048)
-            return rows_k<WT, YT, kTeamGroup, 4, STABLE>(a, 1024, stream);
+    if constexpr (STABLE) {
+        if (vectors <= 256)
+            return rows_k<WT, YT, kTeamGroup4, 1, true>(a, threads_of(vectors), stream);
+        if (vectors <= 512)
+            return rows_k<WT, YT, kTeamGroup4, 2, true>(a, threads_of(vectors, 2), stream);
+        if (vectors <= 1024)
+            return rows_k<WT, YT, kTeamGroup4, 4, true>(a, threads_of(vectors, 4), stream);
+        if constexpr (V == 4) {
+            if (vectors > 2048)
+                return rows_k<WT, YT, kTeamGroup, 4, true>(a, 1024, stream);
+        }
+        return rows_k<WT, YT, kTeamGroup, 2, true>(a, threads_of(vectors, 2), stream);
+    } else {
+        if (vectors <= 1024)
+            return rows_k<WT, YT, kTeamGroup, 1, false>(a, threads_of(vectors), stream);
+        return rows_k<WT, YT, kTeamGroup, 2, false>(a, 1024, stream);
     }
-    return rows_k<WT, YT, kTeamGroup, 2, STABLE>(a, 1024, stream);
 }
 
-template <int WT, int YT, int TEAM>
-void lookup_k(const LookupArgs &a, int threads, hipStream_t stream)
+template <int WT, int YT, int TEAM, int K, int R>
+void lookup_k(const LookupArgs &a, hipStream_t stream)
 {
     constexpr int V = vec_of<WT, YT>;
-    const int64_t per = teams_of<TEAM> * kLookups;
+    const int64_t per = teams_of<TEAM> * R;
     const int64_t groups = (a.count + per - 1) / per;
     const dim3 grid((unsigned)(groups < (1 << 16) ? groups : (1 << 16)),
-                    slabs_of<V>(a.dim, (int64_t)threads / teams_of<TEAM> * V));
+                    slabs_of<V>(a.dim, (int64_t)256 / teams_of<TEAM> * K * V)), block(256);
     if (a.dim % V == 0)
-        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, false>), grid, dim3((unsigned)threads), 0,
-                           stream, a);
+        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, K, R, false>), grid, block, 0, stream, a);
     else
-        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, true>), grid, dim3((unsigned)threads), 0,
-                           stream, a);
+        hipLaunchKernelGGL((lookup_kernel<WT, YT, TEAM, K, R, true>), grid, block, 0, stream, a);
 }
 
 template <int WT, int YT>
@@ -701,11 +736,15 @@ hipError_t lookup(const LookupArgs &a, hipStream_t stream)
 {
     const int64_t vectors = a.dim / vec_of<WT, YT>;
     if (vectors <= 16)
-        lookup_k<WT, YT, kTeam16>(a, 256, stream);
+        lookup_k<WT, YT, kTeam16, 1, 4>(a, stream);
     else if (vectors <= 64)
-        lookup_k<WT, YT, kTeamWave>(a, 256, stream);
+        lookup_k<WT, YT, kTeamWave, 1, 4>(a, stream);
+    else if (vectors <= 128)
+        lookup_k<WT, YT, kTeamWave, 2, 2>(a, stream);
+    else if (vectors <= 256)
+        lookup_k<WT, YT, kTeamWave, 4, 1>(a, stream);
     else
-        lookup_k<WT, YT, kTeamGroup>(a, vectors < 512 ? threads_of(vectors) : 512, stream);
+        lookup_k<WT, YT, kTeamWave, 8, 1>(a, stream);
     return hipGetLastError();
 }
 

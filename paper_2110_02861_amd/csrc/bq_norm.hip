@@ -35,7 +35,10 @@ constexpr float kNaN = __builtin_nanf("");
 //   32768 x 1024 bf16 (128)          wave, 2: 27   4 waves, 1: 31   2: 28
 //   16384 x 4096 bf16 (512)          wave, 8: 61   4 waves, 2: 57   4: 54   8 waves, 1: 63
 //    4096 x 8192 bf16 (1024)         4 waves, 4: 29   8: 37         16 waves, 1: 43
-// A row's own wave needs no barrier; above 4 vectors per lane its registers cost more.
+// A row's own wave needs no barrier; above 4 vectors per lane its registers cost more,
+// but not where rows are looked up (their loads take longer): 32768 tokens of 1600 fp32
+// (400 vectors)                       wave, 8: 72   4 waves, 2: 87   4: 70
+// and with the results streamed past the caches      56               86   63
 // ---------------------------------------------------------------------------
 
 template <int XT, int PT, int YT, bool GATHER, int TEAM, int K, int R, bool TAIL>
@@ -52,6 +55,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
     const int64_t n = a.cols;
     const C c(n, lane, lanes);
     const float rn = 1.0f / (float)n;
+    const bool streams = GATHER && stream_lookup(a.rows * n * elem_bytes<YT>);
     RawRow<PT, V, K, TAIL> pw, pb;
     if (a.weight)
         load_row<PT, false>(c, a.weight, pw);
@@ -148,7 +152,12 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
                 if (GATHER && !known[j])
                     y[e] = kNaN;
             }
-            store_row<YT>(c, row_of<YT>(a.y, row, n), y);
+            // (a long lookup's results would push the table out of the caches; a plain layer
+            // norm's stay there for whoever reads them next)
+            if (GATHER && streams)
+                store_row<YT, true>(c, row_of<YT>(a.y, row, n), y);
+            else
+                store_row<YT>(c, row_of<YT>(a.y, row, n), y);
         }
     }
 }
@@ -264,6 +273,8 @@ hipError_t forward(const NormArgs &a, hipStream_t stream)
         forward_k<XT, PT, YT, GATHER, kTeamWave, 2, 2>(a, 256, stream);
     else if (vectors <= 256)
         forward_k<XT, PT, YT, GATHER, kTeamWave, 4, 1>(a, 256, stream);
+    else if (GATHER && vectors <= 512)
+        forward_k<XT, PT, YT, GATHER, kTeamWave, 8, 1>(a, 256, stream);
     else if (vectors <= 512)
         forward_k<XT, PT, YT, GATHER, kTeamGroup4, 2, 1>(a, threads_of(vectors, 2), stream);
     else if (vectors <= 1024)
@@ -500,9 +511,20 @@ __global__ __launch_bounds__(64 * kSumWaves) void param_grads_kernel(const float
     const int which = blockIdx.y;
     float s = 0.0f;
     if (c < cols) {
-#pragma unroll 16
-        for (int64_t g = wave; g < groups; g += kSumWaves)
-            s += G(partials)[(2 * g + which) * cols + c];
+        constexpr int kBatch = 8;  // in flight
+        for (int64_t g0 = wave; g0 < groups; g0 += kSumWaves * kBatch) {
+            float v[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                const int64_t g = g0 + j * kSumWaves;
+                v[j] = 0.0f;
+                if (g < groups)
+                    v[j] = G(partials)[(2 * g + which) * cols + c];
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+                s += v[j];
+        }
     }
     part[wave][lane] = s;
     __syncthreads();
