@@ -269,6 +269,32 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
     const uint32_t mask = (uint32_t)n - 1;
     const uint32_t *const hist = a.hist;
 
+    // the first subtile's pairs, on their way during the count of places; a wave takes
+    // kSortItems rounds of 64 consecutive pairs
+    const int64_t begin = blockIdx.x * a.tile;
+    const int64_t end = begin + a.tile < a.count ? begin + a.tile : a.count;
+    uint32_t key[kSortItems], pos[kSortItems];
+    bool live[kSortItems];
+    const auto fetch = [&](int64_t sub) {
+#pragma unroll
+        for (int k = 0; k < kSortItems; ++k) {
+            const int64_t i = sub + wave * (64 * kSortItems) + k * 64 + lane;
+            live[k] = i < end;
+            key[k] = 0;
+            pos[k] = (uint32_t)i;
+            if (live[k]) {
+                if (a.pass == 0) {
+                    key[k] = key_at(a, i);
+                } else {
+                    const uint2 v = a.in[i];
+                    key[k] = v.x;
+                    pos[k] = v.y;
+                }
+            }
+        }
+    };
+    fetch(begin);
+
     // the digits' counts in all tiles, and in the tiles before this one: where there
     // are fewer digits than threads, the threads of a digit share the tiles
     for (int d = threadIdx.x; d < n; d += kSortThreads)
@@ -310,33 +336,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
         }
     }
 
-    const int64_t begin = blockIdx.x * a.tile;
-    const int64_t end = begin + a.tile < a.count ? begin + a.tile : a.count;
     for (int64_t sub = begin; sub < end; sub += kSubtile) {
         __syncthreads();  // place is up to date, count has been read
-        for (int i = threadIdx.x; i < kSortWaves * n; i += kSortThreads)
-            count[i / n][i % n] = 0;
+        for (int i = threadIdx.x; i < kSortWaves << a.bits; i += kSortThreads)
+            count[i >> a.bits][i & mask] = 0;
         __syncthreads();
-        uint32_t key[kSortItems], pos[kSortItems], rank[kSortItems];
-        bool live[kSortItems];
-        // a wave takes kSortItems rounds of 64 consecutive pairs
-#pragma unroll
-        for (int k = 0; k < kSortItems; ++k) {
-            const int64_t i = sub + wave * (64 * kSortItems) + k * 64 + lane;
-            live[k] = i < end;
-            key[k] = 0;
-            pos[k] = 0;
-            if (live[k]) {
-                if (a.pass == 0) {
-                    key[k] = key_at(a, i);
-                    pos[k] = (uint32_t)i;
-                } else {
-                    const uint2 v = a.in[i];
-                    key[k] = v.x;
-                    pos[k] = v.y;
-                }
-            }
-        }
+        uint32_t rank[kSortItems];
 #pragma unroll
         for (int k = 0; k < kSortItems; ++k)
             rank[k] = wave_rank((key[k] >> shift) & mask, live[k], a.bits, count[wave]);
@@ -360,6 +365,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
                 a.out[at] = uint2{key[k], pos[k]};
             }
         }
+        if (sub + kSubtile < end)
+            fetch(sub + kSubtile);
     }
 }
 
@@ -370,6 +377,19 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const SortArgs
 
 constexpr int kChunk = 32;
 constexpr int kBatch = 8;  // rows in flight per thread
+
+// Where rows have thousands of tokens, kSpan chunks of one row are added up too: 2^18
+// tokens or more (frequent words), or 32 for every row.  Elsewhere another launch (3 us)
+// is not repaid.  Backward passes, plain / stable, us, without | with: 500,000 tokens,
+// 50257 rows of 128 fp32 184 / 209 | 147 / 175; 60,000 tokens, 300 rows of 1600 fp32
+// 131 / 152 | 126 / 132; 131,072 tokens, 50257 rows of 1024 152 / 210 | 145 / 214;
+// 65,536 tokens, 50257 rows of 1600 154 / 210 | 160 / 210; 5000 tokens, 50 rows of 512
+// 22 / 27 | 24 / 29.
+constexpr int kSpan = 32;
+bool use_spans(int64_t count, int64_t num)
+{
+    return count >= (int64_t{1} << 18) || (count >= (int64_t{1} << 15) && count >= 32 * num);
+}
 
 // What an earlier launch wrote, read by scalar loads where a wave's lanes agree.
 typedef const __attribute__((address_space(4))) uint32_t *cptr;
@@ -384,6 +404,7 @@ struct GradArgs {
     const uint2 *sorted;
     uint32_t *starts;  // num + 1: first position of a key >= i
     float *chunks;     // count / kChunk x dim
+    float *spans;      // count / (kChunk kSpan) x dim, or null
     float *partials;   // stable: groups x 2 x dim
     int32_t chunk_groups;
 };
@@ -449,6 +470,27 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
             for (int i = 0; i < kChunk; ++i)
                 s += load1<YT>(row_of<YT>(a.g.dout, at[i], a.g.dim), col);
             out[col] = s;
+        }
+    }
+}
+
+// Sums of kSpan chunks of one row.
+__global__ __launch_bounds__(256) void span_kernel(const GradArgs a)
+{
+    constexpr int64_t kTokens = kChunk * kSpan;
+    const int64_t n = a.g.count / kTokens;
+    for (int64_t c = blockIdx.x; c < n; c += gridDim.x) {
+        const uint32_t key = a.sorted[c * kTokens].x;
+        if (key != a.sorted[c * kTokens + kTokens - 1].x || (int64_t)key >= a.g.num ||
+            (!a.g.table && (int64_t)key == a.g.padding))
+            continue;
+        const float *const from = a.chunks + c * kSpan * a.g.dim;
+        for (int64_t col = threadIdx.x; col < a.g.dim; col += 256) {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kSpan; ++i)
+                s += G(from)[i * a.g.dim + col];
+            a.spans[c * a.g.dim + col] = s;
         }
     }
 }
@@ -549,14 +591,22 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
         }
         tokens(begin, chunks ? first * kChunk : end);
         if (chunks) {
-            uint32_t i = first;
-            const auto chunk = [&](uint32_t k) {
-                return (const void *)(a.chunks + (int64_t)k * dim);
+            const auto sums = [&](const float *parts, uint32_t i, uint32_t to) {
+                const auto part = [&](uint32_t k) {
+                    return (const void *)(parts + (int64_t)k * dim);
+                };
+                for (; i + B <= to; i += B)
+                    add_rows<kF32, B>(c, s, [&](int j) { return part(i + j); });
+                for (; i < to; ++i)
+                    add_rows<kF32, 1>(c, s, [&](int) { return part(i); });
             };
-            for (; i + B <= last; i += B)
-                add_rows<kF32, B>(c, s, [&](int j) { return chunk(i + j); });
-            for (; i < last; ++i)
-                add_rows<kF32, 1>(c, s, [&](int) { return chunk(i); });
+            const uint32_t span = (first + kSpan - 1) / kSpan, past = last / kSpan;
+            const bool spans = a.spans && span < past;
+            sums(a.chunks, first, spans ? span * kSpan : last);
+            if (spans) {
+                sums(a.spans, span, past);
+                sums(a.chunks, past * kSpan, last);
+            }
             tokens(last * kChunk, end);
         }
         void *const to = row_of<WT>(a.g.dtable, exists ? row : 0, dim);
@@ -635,7 +685,7 @@ constexpr int64_t kRowGroups = 8192;
 constexpr int64_t stable_groups(int64_t dim) { return dim <= 1024 ? 2048 : 1024; }
 
 struct Layout {
-    int64_t pairs_a, pairs_b, hist, starts, chunks, partials, bytes;
+    int64_t pairs_a, pairs_b, hist, starts, chunks, spans, partials, bytes;
 };
 Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
 {
@@ -646,7 +696,9 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     l.hist = l.pairs_b + (s.passes > 1 ? round_up(count * 8, 256) : 0);
     l.starts = l.hist + round_up(s.tiles * 4 << s.bits, 256);
     l.chunks = l.starts + round_up((num + 1) * 4, 256);
-    l.partials = l.chunks + round_up(count / kChunk * dim * 4, 256);
+    l.spans = l.chunks + round_up(count / kChunk * dim * 4, 256);
+    l.partials = l.spans + (use_spans(count, num)
+                                ? round_up(count / (kChunk * kSpan) * dim * 4, 256) : 0);
     l.bytes = l.partials + (stable ? stable_groups(dim) * 2 * dim * 4 : 0);
     return l;
 }
@@ -759,6 +811,7 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
     a.sorted = nullptr;
     a.starts = reinterpret_cast<uint32_t *>(g.workspace + l.starts);
     a.chunks = reinterpret_cast<float *>(g.workspace + l.chunks);
+    a.spans = use_spans(g.count, g.num) ? reinterpret_cast<float *>(g.workspace + l.spans) : nullptr;
     a.partials = stable && (g.dweight || g.dbias)
                      ? reinterpret_cast<float *>(g.workspace + l.partials) : nullptr;
 
@@ -797,6 +850,11 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
     hipLaunchKernelGGL(chunk_kernel<YT>,
                        dim3((unsigned)(a.chunk_groups + (g.num + 1 + 255) / 256)), dim3(256), 0,
                        stream, a);
+    if (a.spans) {
+        const int64_t spans = g.count / (kChunk * kSpan);
+        hipLaunchKernelGGL(span_kernel, dim3((unsigned)(spans < 65536 ? spans : 65536)), dim3(256),
+                           0, stream, a);
+    }
 
     if (!stable) {
         rows<WT, YT, false>(a, stream);

@@ -511,7 +511,7 @@ __global__ __launch_bounds__(64 * kSumWaves) void param_grads_kernel(const float
     const int which = blockIdx.y;
     float s = 0.0f;
     if (c < cols) {
-        constexpr int kBatch = 8;  // in flight
+        constexpr int kBatch = 16;  // in flight
         for (int64_t g0 = wave; g0 < groups; g0 += kSumWaves * kBatch) {
             float v[kBatch];
 #pragma unroll

@@ -102,6 +102,20 @@ def test_one_row_for_all_tokens(count):
         check_lookup(w, ids, F32, 1.0, padding=row)
 
 
+@pytest.mark.parametrize("count", [32767, 32768, 50001])
+def test_thousands_of_tokens_in_a_row(count):
+    """Rows of a few whole spans of chunks, with chunks and tokens on both sides of them."""
+    w = normal((40, 70), 1)
+    say("embedding spans", count)
+    check_lookup(w, word_ids(count, 40, 1), F32, 1.0)
+    check_lookup(w, word_ids(count, 40, 2), BF16, 1.0, padding=1)
+    ids = torch.full((count,), 20, device="cuda")
+    ids[::5000] = 3
+    check_lookup(w, ids, F32, 1.0)
+    check_lookup(w, ids, F32, 1.0, padding=20)
+    check_stable(w, ids, None, None, F32, padding=20)
+
+
 def test_a_million_tokens():
     say("embedding a million tokens")
     w = normal((50257, 8), 1)
