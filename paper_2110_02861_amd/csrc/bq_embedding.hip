@@ -537,9 +537,12 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
     const C c(dim, lane, lanes, (int64_t)blockIdx.y * lanes * K * V);
     const float rn = 1.0f / (float)dim;
     float dw[E], db[E];
+    RawRow<WT, V, K, TAIL> weight;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         dw[e] = db[e] = 0.0f;
+    if (STABLE && a.g.weight)
+        load_row<WT, false>(c, a.g.weight, weight);
 
     // where a row's tokens are, asked for a round ahead
     const auto places = [&](int64_t row, uint32_t &begin, uint32_t &end) {
@@ -649,7 +652,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
             for (int e = 0; e < E; ++e)
                 w[e] = 1.0f;
             if (a.g.weight)
-                load_floats<WT, V, K, TAIL>(c, a.g.weight, w);
+                unpack<WT, V, K, TAIL>(weight, w);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 x[e] = (x[e] - delta) * rstd;
