@@ -604,7 +604,8 @@ bq_status bq_grad_norm(const bq_grad *grads, int32_t ngrads, bq_norm kind, void 
  * The norm as above, then every gradient in place times
  *   c = min(1, max_norm / (norm + 1e-6)),
  * formed in fp64 and rounded to fp32; each product is rounded once to the
- * gradient's type.  Where c is 1 the gradients are left as they are.  A norm
+ * gradient's type.  Where c is 1 the gradients are left as they are.  The
+ * gradients must not overlap (each would be multiplied more than once).  A norm
  * that is infinite makes c 0, a NaN makes it NaN, as IEEE arithmetic has it.
  * The host reads nothing: the call can be captured into a graph.
  * Errors: as bq_grad_norm; BQ_ERR_ARG (max_norm negative or NaN).

@@ -188,7 +188,7 @@ def host():
             for bind, names in ((_bqhost.bind, _HOST_CALLS), (_bqhost.bind_ops, _HOST_OPS)):
                 bind(tuple(ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in names))
             _host_module = _bqhost
-        except ImportError as e:
+        except (ImportError, AttributeError) as e:  # absent, or of other sources
             _host_module = _PythonOnly()
             warnings.warn(f"_bqhost is not available, calls take more host time ({e}); run "
                           "`python -m paper_2110_02861_amd.build`", RuntimeWarning, stacklevel=3)
@@ -711,6 +711,14 @@ def _empty(shape, dtype, device, other):
     return t
 
 
+def _used(other, *tensors):
+    """Keeps the memory of a call's inputs until stream `other` has used them."""
+    if other is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(other)
+
+
 def _output(out, shape, dtype, device, other, name):
     if out is None:
         return _empty(shape, dtype, device, other)
@@ -760,6 +768,7 @@ def bq_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, stats: b
     xt = _dtype_id(x, "x")
     pdtype, w, b = _norm_params(x, weight, bias, cols)
     other = _other(stream)
+    _used(other, x, weight, bias)
     y = _output(out, x.shape, x.dtype, x.device, other, "out")
     mean = rstd = None
     if stats:
@@ -795,6 +804,7 @@ def bq_layer_norm_backward(dy, x, weight, mean, rstd, need_dx: bool = True,
     if m is None or r is None:
         raise TypeError("mean and rstd are required")
     other = _other(stream)
+    _used(other, dy, x, weight, mean, rstd)
     dx = _empty(x.shape, x.dtype, x.device, other) if need_dx else None
     dw = db = ws = None
     if need_params:
@@ -856,7 +866,9 @@ def bq_embedding_forward(weight, ids, scale: float = 1.0, out_dtype=None, out=No
     wt, num, dim = _table_of(weight)
     ptr, bits = _ids_of(ids)
     dtype = _lookup_dtype(weight.dtype, out_dtype)
-    y = _output(out, (*ids.shape, dim), dtype, weight.device, _other(stream), "out")
+    other = _other(stream)
+    _used(other, weight, ids)
+    y = _output(out, (*ids.shape, dim), dtype, weight.device, other, "out")
     _check(lib().bq_embedding_forward(wt, _dtype_id(dtype, "out"), weight.data_ptr(), num, dim, ptr,
                                       bits, ids.numel(), scale, y.data_ptr(), _stream(stream)),
            "bq_embedding_forward")
@@ -883,6 +895,7 @@ def bq_embedding_backward(dout, ids, num: int, padding_idx=None, scale: float = 
     _lookup_dtype(dtype, dout.dtype)
     pad = _padding(padding_idx, num)
     other = _other(stream)
+    _used(other, dout, ids)
     dw = _output(out, (num, dim), dtype, dout.device, other, "out")
     ws = _workspace(workspace, lib().bq_embedding_workspace_bytes(ids.numel(), num, dim),
                     dout.device, other)
@@ -906,7 +919,9 @@ def bq_stable_embedding_forward(weight, ids, norm_weight=None, norm_bias=None, e
     dtype = _lookup_dtype(weight.dtype, out_dtype)
     w = _vector(norm_weight, dim, weight.dtype, "norm_weight")
     b = _vector(norm_bias, dim, weight.dtype, "norm_bias")
-    y = _output(out, (*ids.shape, dim), dtype, weight.device, _other(stream), "out")
+    other = _other(stream)
+    _used(other, weight, ids, norm_weight, norm_bias)
+    y = _output(out, (*ids.shape, dim), dtype, weight.device, other, "out")
     _check(lib().bq_stable_embedding_forward(wt, _dtype_id(dtype, "out"), weight.data_ptr(), num,
                                              dim, ptr, bits, ids.numel(), w, b, eps, y.data_ptr(),
                                              _stream(stream)), "bq_stable_embedding_forward")
@@ -924,6 +939,7 @@ def bq_stable_embedding_backward(dout, ids, weight, norm_weight=None, eps: float
     w = _vector(norm_weight, dim, weight.dtype, "norm_weight")
     pad = _padding(padding_idx, num)
     other = _other(stream)
+    _used(other, dout, ids, weight, norm_weight)
     dweight = _empty((num, dim), weight.dtype, weight.device, other)
     dw = db = None
     if need_norm:
@@ -977,7 +993,12 @@ def _grad_norm(grads, norm_type, max_norm, out, workspace, stream):
     kind = _norm_kind(norm_type)
     grads = list(grads)
     arr = make_grad_array(grads)
+    if max_norm is not None:
+        places = [g.data_ptr() for g in grads if g.numel()]
+        if len(set(places)) != len(places):
+            raise ValueError("two gradients are in the same place")
     other = _other(stream)
+    _used(other, *grads)
     device = torch.device("cuda", torch.cuda.current_device())
     norm = _output(out, (), torch.float32, device, other, "out")
     ws = _workspace(workspace, lib().bq_grad_norm_workspace_bytes(len(grads)), device, other)
@@ -999,5 +1020,5 @@ def bq_grad_norm(grads, norm_type=2.0, out=None, workspace=None, stream=None):
 def bq_clip_grad_norm(grads, max_norm: float, norm_type=2.0, out=None, workspace=None,
                       stream=None):
     """The norm as bq_grad_norm; then every gradient times min(1, max_norm / (norm + 1e-6)),
-    in place.  Nothing is read back by the host."""
+    in place.  The gradients must not overlap.  Nothing is read back by the host."""
     return _grad_norm(grads, norm_type, float(max_norm), out, workspace, stream)

@@ -60,17 +60,17 @@ bool modes()
                c10::DispatchKey::FuncTorchDynamicLayerFrontMode);
 }
 
-// Lets other Python threads run during a call; a no-op in the engine's threads, which
-// do not hold the interpreter.
-struct Unlocked {
-    PyThreadState *save;
-    Unlocked() : save(PyGILState_Check() ? PyEval_SaveThread() : nullptr) {}
-    ~Unlocked()
-    {
-        if (save)
-            PyEval_RestoreThread(save);
-    }
-};
+// Runs f without the interpreter lock, which the functions below hold when Python calls
+// them; the engine calls the backward passes without it.
+template <class F>
+auto unlocked(F f)
+{
+    struct Lock {
+        PyThreadState *save = PyEval_SaveThread();
+        ~Lock() { PyEval_RestoreThread(save); }
+    } lock;
+    return f();
+}
 
 void succeed(bq_status s, const char *what)
 {
@@ -197,7 +197,6 @@ at::Tensor norm_forward(const at::Tensor &x, const at::Tensor &w, const at::Tens
     }
     const bq_dtype xt = dtype_of(x.scalar_type()), wt = dtype_of(pt);
     const hipStream_t stream = current(x);
-    const Unlocked unlocked;
     succeed(lib.norm_forward(xt, wt, data(x), r.rows, r.cols, r.stride, data(w), data(b),
                              static_cast<float>(eps), data(y),
                              static_cast<float *>(mean ? data(*mean) : nullptr),
@@ -238,7 +237,6 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
                 db = at::empty({r.cols}, x.options().dtype(pt));
             ws = at::empty({lib.norm_workspace(r.rows, r.cols)}, x.options().dtype(at::kByte));
         }
-        const Unlocked unlocked;
         succeed(lib.norm_backward(dtype_of(x.scalar_type()), dtype_of(pt), data(dy), g.stride,
                                   data(x), r.stride, r.rows, r.cols, data(w),
                                   static_cast<const float *>(data(saved[2])),
@@ -268,9 +266,11 @@ PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const at::Tensor w = vector(args[1], cols, pt, device);
         const at::Tensor b = vector(args[2], cols, pt, device);
         const double eps = real(args[3]);
-        if (truth(args[4]) && wants_grad({&x, &w, &b}))
-            return THPVariable_Wrap(LayerNorm::apply(x, w, b, eps));
-        return THPVariable_Wrap(norm_forward(x, w, b, eps, nullptr, nullptr));
+        const bool grads = truth(args[4]) && wants_grad({&x, &w, &b});
+        return THPVariable_Wrap(unlocked([&] {
+            return grads ? LayerNorm::apply(x, w, b, eps)
+                         : norm_forward(x, w, b, eps, nullptr, nullptr);
+        }));
     });
 }
 
@@ -291,7 +291,6 @@ at::Tensor lookup_forward(const at::Tensor &ids, const at::Tensor &w, double sca
                           at::ScalarType out)
 {
     at::Tensor y = at::empty(output_sizes(ids, w), w.options().dtype(out));
-    const Unlocked unlocked;
     succeed(lib.lookup(dtype_of(w.scalar_type()), dtype_of(out), data(w), w.size(0), w.size(1),
                        data(ids), id_bits(ids), ids.numel(), static_cast<float>(scale), data(y),
                        current(w)),
@@ -323,7 +322,6 @@ struct Embedding : torch::autograd::Function<Embedding> {
         at::Tensor dw = at::empty({num, dim}, dy.options().dtype(type));
         at::Tensor ws = at::empty({lib.lookup_workspace(ids.numel(), num, dim)},
                                   dy.options().dtype(at::kByte));
-        const Unlocked unlocked;
         succeed(lib.lookup_backward(dtype_of(type), dtype_of(dy.scalar_type()), data(dy), data(ids),
                                     id_bits(ids), ids.numel(), num, dim,
                                     ctx->saved_data["padding"].toInt(), scale, data(dw), data(ws),
@@ -372,10 +370,12 @@ PyObject *embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             return none();
         const Lookup l = lookup_of(args[0], args[1], args[2], args[4], c10::hip::current_device());
         const double scale = real(args[3]);
-        if (truth(args[5]) && wants_grad({&l.w}))
-            return THPVariable_Wrap(
-                Embedding::apply(l.ids, l.w, l.padding, scale, static_cast<int64_t>(l.out)));
-        return THPVariable_Wrap(lookup_forward(l.ids, l.w, scale, l.out));
+        const bool grads = truth(args[5]) && wants_grad({&l.w});
+        return THPVariable_Wrap(unlocked([&] {
+            return grads ? Embedding::apply(l.ids, l.w, l.padding, scale,
+                                            static_cast<int64_t>(l.out))
+                         : lookup_forward(l.ids, l.w, scale, l.out);
+        }));
     });
 }
 
@@ -383,7 +383,6 @@ at::Tensor stable_forward(const at::Tensor &ids, const at::Tensor &w, const at::
                           const at::Tensor &nb, double eps, at::ScalarType out)
 {
     at::Tensor y = at::empty(output_sizes(ids, w), w.options().dtype(out));
-    const Unlocked unlocked;
     succeed(lib.stable(dtype_of(w.scalar_type()), dtype_of(out), data(w), w.size(0), w.size(1),
                        data(ids), id_bits(ids), ids.numel(), data(nw), data(nb),
                        static_cast<float>(eps), data(y), current(w)),
@@ -419,16 +418,13 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
             dnb = at::empty({dim}, w.options());
         at::Tensor ws = at::empty({lib.stable_workspace(ids.numel(), num, dim)},
                                   w.options().dtype(at::kByte));
-        {
-            const Unlocked unlocked;
-            succeed(lib.stable_backward(
-                        dtype_of(w.scalar_type()), dtype_of(dy.scalar_type()), data(dy), data(ids),
-                        id_bits(ids), ids.numel(), data(w), num, dim,
-                        ctx->saved_data["padding"].toInt(), data(nw),
-                        static_cast<float>(ctx->saved_data["eps"].toDouble()), data(dw), data(dnw),
-                        data(dnb), data(ws), current(w)),
-                    "bq_stable_embedding_backward");
-        }
+        succeed(lib.stable_backward(
+                    dtype_of(w.scalar_type()), dtype_of(dy.scalar_type()), data(dy), data(ids),
+                    id_bits(ids), ids.numel(), data(w), num, dim,
+                    ctx->saved_data["padding"].toInt(), data(nw),
+                    static_cast<float>(ctx->saved_data["eps"].toDouble()), data(dw), data(dnw),
+                    data(dnb), data(ws), current(w)),
+                "bq_stable_embedding_backward");
         if (!need_w)
             dw = at::Tensor();
         return once({at::Tensor(), dw, dnw, dnb, at::Tensor(), at::Tensor(), at::Tensor()});
@@ -448,10 +444,12 @@ PyObject *stable_embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const at::Tensor nw = vector(args[2], l.w.size(1), l.w.scalar_type(), device);
         const at::Tensor nb = vector(args[3], l.w.size(1), l.w.scalar_type(), device);
         const double eps = real(args[4]);
-        if (truth(args[7]) && wants_grad({&l.w, &nw, &nb}))
-            return THPVariable_Wrap(StableEmbedding::apply(l.ids, l.w, nw, nb, eps, l.padding,
-                                                           static_cast<int64_t>(l.out)));
-        return THPVariable_Wrap(stable_forward(l.ids, l.w, nw, nb, eps, l.out));
+        const bool grads = truth(args[7]) && wants_grad({&l.w, &nw, &nb});
+        return THPVariable_Wrap(unlocked([&] {
+            return grads ? StableEmbedding::apply(l.ids, l.w, nw, nb, eps, l.padding,
+                                                  static_cast<int64_t>(l.out))
+                         : stable_forward(l.ids, l.w, nw, nb, eps, l.out);
+        }));
     });
 }
 
@@ -495,7 +493,8 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             if (!exact)
                 return none();
             dense(g, device);
-            need(one_range(g));
+            // (two gradients in the same place: Python refuses to clip them)
+            need(one_range(g) && (g.numel() == 0 || !clips || seen.insert(g.data_ptr()).second));
             list.push_back({g.data_ptr(), g.numel(), dtype_of(g.scalar_type())});
             grads.push_back(g);
         }
@@ -505,12 +504,11 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         at::Tensor ws = at::empty({lib.clip_workspace(count)}, grads[0].options().dtype(at::kByte));
         const hipStream_t stream = current(norm);
         float *const out = static_cast<float *>(norm.data_ptr());
-        {
-            const Unlocked unlocked;
-            succeed(clips ? lib.clip(list.data(), count, kind, max_norm, ws.data_ptr(), out, stream)
-                          : lib.grad_norm(list.data(), count, kind, ws.data_ptr(), out, stream),
-                    "the gradient norm");
-        }
+        const bq_status status = unlocked([&] {
+            return clips ? lib.clip(list.data(), count, kind, max_norm, ws.data_ptr(), out, stream)
+                         : lib.grad_norm(list.data(), count, kind, ws.data_ptr(), out, stream);
+        });
+        succeed(status, "the gradient norm");
         if (clips)
             for (const at::Tensor &g : grads)
                 if (!g.is_inference())

@@ -21,9 +21,9 @@ bool elements(const void *p, bq_dtype d) { return aligned(p, bytes_of(d)); }
 
 bq_status from_hip(hipError_t e) { return e == hipSuccess ? BQ_OK : BQ_ERR_HIP; }
 
-// Byte offsets stay far below 2^63, and a row's length below 2^31.
+// Byte offsets stay far below 2^63, and the launches below 2^32 work-items.
 constexpr int64_t kMaxRows = int64_t{1} << 40;
-constexpr int64_t kMaxCols = int64_t{1} << 30;
+constexpr int64_t kMaxCols = int64_t{1} << 27;
 constexpr int64_t kMaxDim = int64_t{1} << 24;  // at most 2^16 slabs of a launch
 
 bq_status check_norm(bq_dtype dtype, bq_dtype param_dtype, int64_t rows, int64_t cols, float eps)

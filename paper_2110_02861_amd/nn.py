@@ -5,8 +5,10 @@ Section 3.3, and the layer norm and embedding that it is made of, in HIP kernels
 libbq's kernels (``bq.bq_layer_norm_forward`` and its kin), ``LayerNorm`` and ``Embedding``
 the modules, with the parameters, names and initial values of torch's.  They take GPU
 tensors in fp32, fp16 or bf16 and raise for others: there is no CPU fallback.  Gradients
-are of first order, and the same bits every time.  ``StableEmbedding`` runs in plain
-torch unless it is built with ``fused=True``.
+are of first order, and the same bits every time.  A training step is captured into a graph
+like one of torch's own layers: backward passes on a side stream, and no graph of an
+eager pass over the same leaves still alive.  ``StableEmbedding`` runs in plain torch
+unless it is built with ``fused=True``.
 
 The stable embedding: a word embedding initialized with Xavier-uniform values whose output goes
 through a layer norm (add position embeddings after it).  Its weight carries

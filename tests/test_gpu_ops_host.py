@@ -208,6 +208,13 @@ def test_clip_agrees(native, monkeypatch, handled):
     assert all(p.grad._version > v for p, v in zip(params[:-1], versions))
     with pytest.raises(ValueError):
         optim.clip_grad_norm_(params, 1.0, norm_type=1.0)
+    params[0].grad = normal((30, 40), 6)
+    other = torch.nn.Parameter(normal((1200,), 4))
+    other.grad = params[0].grad.view(1200)
+    kept = other.grad.clone()
+    with pytest.raises(ValueError, match="same place"):
+        optim.clip_grad_norm_([params[0], other], 1.0)
+    assert torch.equal(kept, other.grad)
     params[0].grad = normal((30, 80), 3)[:, ::2]
     with pytest.raises(ValueError):
         optim.clip_grad_norm_(params, 1.0)
