@@ -188,9 +188,18 @@ __device__ inline double join(const double *partials, int n, bool inf_norm)
 {
     __shared__ double part[kThreads / 64];
     double v = 0.0;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const double x = G(partials)[i];
-        v = inf_norm ? (x > v || x != x ? x : v) : v + x;
+    constexpr int kBatch = 8;  // in flight
+    for (int i = threadIdx.x; i < n; i += kThreads * kBatch) {
+        double x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            x[j] = 0.0;
+            if (i + j * kThreads < n)
+                x[j] = G(partials)[i + j * kThreads];
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            v = inf_norm ? (x[j] > v || x[j] != x[j] ? x[j] : v) : v + x[j];
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {

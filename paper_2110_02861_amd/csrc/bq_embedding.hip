@@ -410,12 +410,12 @@ struct GradArgs {
 };
 
 template <int YT>
-__global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
+__global__ __launch_bounds__(512) void chunk_kernel(const GradArgs a)
 {
     constexpr int V = elem_bytes<YT> == 4 ? 4 : 8;
     __shared__ uint32_t at[kChunk];
     if ((int)blockIdx.x >= a.chunk_groups) {
-        const int64_t row = (int64_t)(blockIdx.x - a.chunk_groups) * 256 + threadIdx.x;
+        const int64_t row = (int64_t)(blockIdx.x - a.chunk_groups) * blockDim.x + threadIdx.x;
         if (row > a.g.num)
             return;
         uint32_t lo = 0, hi = (uint32_t)a.g.count;
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256) void chunk_kernel(const GradArgs a)
         __syncthreads();
         float *const out = a.chunks + c * a.g.dim;
         const int64_t whole = a.g.dim / V * V;
-        for (int64_t col = (int64_t)threadIdx.x * V; col < whole; col += 256 * V) {
+        for (int64_t col = (int64_t)threadIdx.x * V; col < whole; col += blockDim.x * V) {
             float s[V];
 #pragma unroll
             for (int r = 0; r < V; ++r)
@@ -850,9 +850,12 @@ hipError_t backward(const LookupGradArgs &g, hipStream_t stream)
     }
     const int64_t chunks = g.count / kChunk;
     a.chunk_groups = (int32_t)(chunks < 65536 ? chunks : 65536);
+    // a thread for every vector of a row, where there are so many
+    const int64_t vectors = g.dim / (elem_bytes<YT> == 4 ? 4 : 8);
+    const int threads = vectors < 64 ? 64 : vectors < 512 ? threads_of(vectors) : 512;
     hipLaunchKernelGGL(chunk_kernel<YT>,
-                       dim3((unsigned)(a.chunk_groups + (g.num + 1 + 255) / 256)), dim3(256), 0,
-                       stream, a);
+                       dim3((unsigned)(a.chunk_groups + (g.num + threads) / threads)),
+                       dim3((unsigned)threads), 0, stream, a);
     if (a.spans) {
         const int64_t spans = g.count / (kChunk * kSpan);
         hipLaunchKernelGGL(span_kernel, dim3((unsigned)(spans < 65536 ? spans : 65536)), dim3(256),

@@ -162,9 +162,10 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_forward_kernel(const 
     }
 }
 
-// Rows too long for the registers of a workgroup: the row is read three times.
+// Rows too long for the registers of a workgroup (above 16384 elements): the row is read
+// three times.
 constexpr int kLongWaves = 16;
-template <int XT, int PT, int YT, bool GATHER>
+template <int XT, int PT, int YT>
 __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(const NormArgs a)
 {
     constexpr int V = vec_of<XT, YT>;
@@ -172,15 +173,7 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
     __shared__ float scratch[3 * 16];
     const int64_t n = a.cols;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        int64_t from = row;
-        bool known = true;
-        if constexpr (GATHER) {
-            from = id_at(a.ids, row, a.ids64);
-            known = from >= 0 && from < a.table_rows;
-            if (!known)
-                from = 0;
-        }
-        const void *const xp = row_of<XT>(a.x, from, a.x_stride);
+        const void *const xp = row_of<XT>(a.x, row, a.x_stride);
         const int64_t c0 = (int64_t)threadIdx.x * V;
         const float rn = 1.0f / (float)n;
         float sum[1] = {0.0f};
@@ -227,11 +220,8 @@ __global__ __launch_bounds__(64 * kLongWaves) void norm_forward_long_kernel(cons
             if (a.bias)
                 load_cols<PT, V>(a.bias, c, n, b);
 #pragma unroll
-            for (int r = 0; r < V; ++r) {
+            for (int r = 0; r < V; ++r)
                 y[r] = __builtin_fmaf(((x[r] - mean0) - delta) * rstd, w[r], b[r]);
-                if (GATHER && !known)
-                    y[r] = kNaN;
-            }
             store_cols<YT, V>(yp, c, n, y);
         }
     }
@@ -260,6 +250,22 @@ int threads_of(int64_t vectors, int k = 1)
     return (int)((vectors + 64 * k - 1) / (64 * k) * 64);
 }
 
+// More than 2048 vectors.
+template <int XT, int PT, int YT, bool GATHER>
+void forward_longest(const NormArgs &a, int64_t vectors, hipStream_t stream)
+{
+    if constexpr (vec_of<XT, YT> == 4) {
+        if (GATHER || vectors <= 4096) {  // (a looked-up row has at most 16384 elements)
+            forward_k<XT, PT, YT, GATHER, kTeamGroup, 4, 1>(a, threads_of(vectors, 4), stream);
+            return;
+        }
+    }
+    if constexpr (!GATHER)
+        hipLaunchKernelGGL((norm_forward_long_kernel<XT, PT, YT>),
+                           dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))),
+                           dim3(64 * kLongWaves), 0, stream, a);
+}
+
 template <int XT, int PT, int YT, bool GATHER>
 hipError_t forward(const NormArgs &a, hipStream_t stream)
 {
@@ -273,21 +279,15 @@ hipError_t forward(const NormArgs &a, hipStream_t stream)
         forward_k<XT, PT, YT, GATHER, kTeamWave, 2, 2>(a, 256, stream);
     else if (vectors <= 256)
         forward_k<XT, PT, YT, GATHER, kTeamWave, 4, 1>(a, 256, stream);
-    else if (GATHER && vectors <= 512)
-        forward_k<XT, PT, YT, GATHER, kTeamWave, 8, 1>(a, 256, stream);
     else if (vectors <= 512)
-        forward_k<XT, PT, YT, GATHER, kTeamGroup4, 2, 1>(a, threads_of(vectors, 2), stream);
+        forward_k<XT, PT, YT, GATHER, GATHER ? kTeamWave : kTeamGroup4, GATHER ? 8 : 2, 1>(
+            a, GATHER ? 256 : threads_of(vectors, 2), stream);
     else if (vectors <= 1024)
         forward_k<XT, PT, YT, GATHER, kTeamGroup4, 4, 1>(a, threads_of(vectors, 4), stream);
     else if (vectors <= 2048)
         forward_k<XT, PT, YT, GATHER, kTeamGroup4, 8, 1>(a, threads_of(vectors, 8), stream);
-    else if (V == 4 && vectors <= 4096)
-        forward_k<XT, PT, YT, GATHER, kTeamGroup, 16 / V, 1>(a, threads_of(vectors, 16 / V),
-                                                             stream);
     else
-        hipLaunchKernelGGL((norm_forward_long_kernel<XT, PT, YT, GATHER>),
-                           dim3((unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20))),
-                           dim3(64 * kLongWaves), 0, stream, a);
+        forward_longest<XT, PT, YT, GATHER>(a, vectors, stream);
     return hipGetLastError();
 }
 
