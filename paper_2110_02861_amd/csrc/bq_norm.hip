@@ -233,7 +233,10 @@ void forward_k(const NormArgs &a, int threads, hipStream_t stream)
     constexpr int V = vec_of<XT, YT>;
     const int64_t rows = teams_of<TEAM> * R;
     const int64_t groups = (a.rows + rows - 1) / rows;
-    const int64_t most = 1024 * 256 / threads;
+    // as many as run at once: where a lane holds 32 values, three workgroups of 256 threads
+    // to a CU (8192 x 1600 fp16 13.5 us with 768, 14.9 with 1024, 16.2 with 2048;
+    // 40000 x 256 fp32 18.3, 17.1, 18.9)
+    const int64_t most = (K * V >= 32 ? 768 : 1024) * 256 / threads;
     const dim3 grid((unsigned)(groups < most ? groups : most)), block((unsigned)threads);
     if (a.cols % V == 0)
         hipLaunchKernelGGL((norm_forward_kernel<XT, PT, YT, GATHER, TEAM, K, R, false>), grid,
