@@ -105,7 +105,7 @@ static_assert(sizeof(ClipArgs) <= 4096, "kernel argument block must stay below 4
 constexpr int kClipTileBytes = 16384;
 // Workgroups of a norm launch, at most: all run at once, five to a CU (the norm of 1.56e9
 // fp16 gradients: 1.11 ms with 256, 0.71 with 512, 0.54 with 1024, 0.52 with 1280 and
-// 1536, 0.54 with 3072).
+// 1536).
 constexpr int kClipMaxGroups = 1280;
 // A clip launch's workgroups each add up the partial sums; above this many, a launch
 // of its own adds them up once (behind the last of them).
