@@ -344,7 +344,8 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_backward_kernel(const
             mean[j] = G(a.mean)[row];
             rstd[j] = G(a.rstd)[row];
         }
-        // behind the row's end dy is 0, and so is everything that is summed
+        // behind the row's end x and dy are 0 (x from no mean: a large one times rstd may be
+        // infinite), and so is everything that is summed
         float x[R][E], dy[R][E];
         float two[2 * R];
 #pragma unroll
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(most_threads<TEAM>) void norm_backward_kernel(const
             unpack<XT, V, K, TAIL>(rg[j], dy[j]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                x[j][e] = (x[j][e] - mean[j]) * rstd[j];
+                x[j][e] = (x[j][e] - (c.valid(e) ? mean[j] : 0.0f)) * rstd[j];
                 if (live) {
                     dw[e] = __builtin_fmaf(dy[j][e], x[j][e], dw[e]);
                     db[e] += dy[j][e];

@@ -114,6 +114,24 @@ def test_constant_rows_and_eps():
     check_all(x * 1e-4, w, b, dy, F32, eps=1e-3)
 
 
+@pytest.mark.parametrize("xt", [F32, BF16])
+def test_gradients_of_large_constant_rows(xt):
+    """Rows of 2^120, whose mean is exact: the mean times rstd is above fp32's largest value,
+    xh is 0."""
+    x = torch.full((5, 32), 2.0 ** 120, device="cuda", dtype=xt)
+    w, dy = 1 + normal((32,), 1, 0.1), normal((5, 32), 2, 0.01).to(xt)
+    _, mean, rstd = bq.bq_layer_norm_forward(x, w, None, EPS, stats=True)
+    say("layer norm large constant rows", xt)
+    got = bq.bq_layer_norm_backward(dy, x, w, mean, rstd)
+    _, xh, mr, rr = ref.layer_norm(x, w, None, EPS)
+    assert not xh.any() and torch.equal(mean.double(), mr[:, 0])
+    want = ref.layer_norm_grads(dy, xh, rr, w)
+    # the saved mean is exact, and takes no part in the bounds
+    bounds = ref.backward_bounds(dy, xh, torch.zeros_like(mr), rr, w, *want, xt, F32)
+    for g, r, e, what in zip(got, want, bounds, ("dx", "dw", "db")):
+        ref.check(g, r, e, what)
+
+
 @pytest.mark.parametrize("cols", [200, 3000, 40000])
 def test_rows_that_are_not_finite_stay_apart(cols):
     x, w, b, dy = inputs(6, cols, F32, F32)
