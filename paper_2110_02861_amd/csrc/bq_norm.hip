@@ -514,6 +514,15 @@ int64_t backward_k(const NormGradArgs &a, int threads, hipStream_t stream)
     return groups;
 }
 
+// Shares of the rows in a launch of norm_params_kernel with `blocks` workgroups to each:
+// eight workgroups to a CU.
+int64_t shares_of(int64_t rows, int64_t blocks)
+{
+    const int64_t shares = (2048 + blocks - 1) / blocks;
+    const int64_t most = rows < kNormGradGroups ? rows : kNormGradGroups;
+    return shares < most ? shares : most;
+}
+
 template <int XT, int PT>
 int64_t backward(const NormGradArgs &a, hipStream_t stream)
 {
@@ -544,9 +553,7 @@ int64_t backward(const NormGradArgs &a, hipStream_t stream)
     if (!a.partials)
         return 0;
     const int64_t blocks = (a.cols + 256 * V - 1) / (256 * V);
-    int64_t shares = (2048 + blocks - 1) / blocks;  // eight workgroups to a CU
-    const int64_t most = a.rows < kNormGradGroups ? a.rows : kNormGradGroups;
-    shares = shares < most ? shares : most;
+    const int64_t shares = shares_of(a.rows, blocks);
     hipLaunchKernelGGL(norm_params_kernel<XT>, dim3((unsigned)blocks, (unsigned)shares), dim3(256),
                        0, stream, a);
     return shares;
@@ -596,7 +603,11 @@ __global__ __launch_bounds__(64 * kSumWaves) void param_grads_kernel(const float
 
 int64_t norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    const int64_t groups = rows < 1 ? 1 : rows < kNormGradGroups ? rows : kNormGradGroups;
+    int64_t groups = rows < 1 ? 1 : rows < kNormGradGroups ? rows : kNormGradGroups;
+    // rows that are too long for registers in every type: the fewest workgroups to a share
+    // are 16-bit rows', 8 elements to a thread
+    if (cols / 8 > 2048 && rows > 0)
+        groups = shares_of(rows, (cols + 2047) / 2048);
     return groups * 2 * cols * 4;
 }
 

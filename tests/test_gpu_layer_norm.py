@@ -115,6 +115,24 @@ def test_constant_rows_and_eps():
 
 
 @pytest.mark.parametrize("xt", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(600, 16384), (600, 16392), (250, 70003)])
+def test_workspace_of_long_rows(rows, cols, xt):
+    """A workspace of the size asked for is enough, and nothing behind it is written."""
+    x, w, b, dy = inputs(rows, cols, xt, F32)
+    _, mean, rstd = bq.bq_layer_norm_forward(x, w, b, EPS, stats=True)
+    need = bq.lib().bq_layer_norm_workspace_bytes(rows, cols)
+    ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device="cuda")
+    say("layer norm workspace", rows, cols, xt)
+    got = bq.bq_layer_norm_backward(dy, x, w, mean, rstd, workspace=ws[:need])
+    assert bool((ws[need:] == 77).all())
+    _, xh, mr, rr = ref.layer_norm(x, w, b, EPS)
+    want = ref.layer_norm_grads(dy, xh, rr, w)
+    for g, r, e, what in zip(got, want, ref.backward_bounds(dy, xh, mr, rr, w, *want, xt, F32),
+                             ("dx", "dw", "db")):
+        ref.check(g, r, e, what)
+
+
+@pytest.mark.parametrize("xt", [F32, BF16])
 def test_gradients_of_large_constant_rows(xt):
     """Rows of 2^120, whose mean is exact: the mean times rstd is above fp32's largest value,
     xh is 0."""

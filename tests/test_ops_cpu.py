@@ -146,6 +146,10 @@ def test_workspace_sizes():
     assert lib.bq_layer_norm_workspace_bytes(10, 0) == 0
     assert lib.bq_layer_norm_workspace_bytes(-1, 8) == 0
     assert lib.bq_layer_norm_workspace_bytes(10, 8) >= 2 * 8 * 4
+    # rows above 16384 elements: fewer partial rows the longer they are
+    assert lib.bq_layer_norm_workspace_bytes(4096, 1 << 20) == 4 * 2 * (1 << 20) * 4
+    assert lib.bq_layer_norm_workspace_bytes(3, 1 << 20) == 3 * 2 * (1 << 20) * 4
+    assert lib.bq_layer_norm_workspace_bytes(1 << 20, 1 << 27) == 2 * (1 << 27) * 4
     assert lib.bq_embedding_workspace_bytes(1 << 31, 10, 8) == 0
     assert lib.bq_embedding_workspace_bytes(10, 0, 8) == 0
     assert lib.bq_stable_embedding_workspace_bytes(10, 10, 16385) == 0
