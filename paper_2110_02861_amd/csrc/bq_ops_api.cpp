@@ -292,7 +292,7 @@ int64_t bq_grad_norm_workspace_bytes(int32_t ngrads)
 {
     if (ngrads < 0)
         return 0;
-    const int64_t launches = (ngrads + bq::kMaxClipTensors - 1) / bq::kMaxClipTensors;
+    const int64_t launches = (int64_t{ngrads} + bq::kMaxClipTensors - 1) / bq::kMaxClipTensors;
     return (launches * bq::kClipMaxGroups + 1) * 8;
 }
 

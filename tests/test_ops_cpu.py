@@ -158,6 +158,7 @@ def test_workspace_sizes():
     assert lib.bq_stable_embedding_workspace_bytes(0, 10, 8) >= 2 * 8 * 4
     assert lib.bq_grad_norm_workspace_bytes(-1) == 0
     assert lib.bq_grad_norm_workspace_bytes(0) == 8
+    assert lib.bq_grad_norm_workspace_bytes((1 << 31) - 1) > (1 << 31) // 180 * 8
     # more than 4 GiB: the sizes are 64-bit
     assert lib.bq_embedding_workspace_bytes((1 << 31) - 1, 50257, 4096) > 1 << 36
     assert ctypes.sizeof(bq.bq_grad) == 24
