@@ -662,6 +662,8 @@ def _on_device(t, name):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided:
         raise TypeError(f"{name} must be a dense GPU torch tensor")
+    if t.is_neg():
+        raise TypeError(f"{name} is a view with a pending negation; pass {name}.resolve_neg()")
     if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
@@ -712,7 +714,7 @@ def _empty(shape, dtype, device, other):
 
 
 def _used(other, *tensors):
-    """Keeps the memory of a call's inputs until stream `other` has used them."""
+    """Keeps the memory of a call's tensors until stream `other` has used them."""
     if other is not None:
         for t in tensors:
             if t is not None:
@@ -727,6 +729,7 @@ def _output(out, shape, dtype, device, other, name):
         raise TypeError(f"{name} must be {dtype}, got {out.dtype}")
     if tuple(out.shape) != tuple(shape) or not out.is_contiguous():
         raise ValueError(f"{name} must be contiguous, of shape {tuple(shape)}")
+    _used(other, out)
     return out
 
 
@@ -741,6 +744,7 @@ def _workspace(workspace, nbytes, device, other):
     if workspace.numel() * workspace.element_size() < nbytes:
         raise ValueError(f"workspace holds {workspace.numel() * workspace.element_size()} bytes, "
                          f"needs {nbytes}")
+    _used(other, workspace)
     return workspace
 
 

@@ -224,7 +224,9 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         const at::DeviceGuard guard(x.device());
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1),
                    need_b = ctx->needs_input_grad(2);
-        const at::Tensor dy = packed_rows(grads[0]) ? grads[0] : grads[0].contiguous();
+        at::Tensor dy = grads[0].resolve_neg();
+        if (!packed_rows(dy))
+            dy = dy.contiguous();
         const auto pt = static_cast<at::ScalarType>(ctx->saved_data["param"].toInt());
         const Rows r = rows_of(x), g = rows_of(dy);
         at::Tensor dx, dw, db, ws;
@@ -315,7 +317,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
     {
         const at::Tensor ids = ctx->get_saved_variables()[0];
         const at::DeviceGuard guard(ids.device());
-        const at::Tensor dy = grads[0].contiguous();
+        const at::Tensor dy = grads[0].resolve_neg().contiguous();
         const int64_t num = ctx->saved_data["num"].toInt(), dim = dy.size(-1);
         const auto type = static_cast<at::ScalarType>(ctx->saved_data["dtype"].toInt());
         const auto scale = static_cast<float>(ctx->saved_data["scale"].toDouble());
@@ -407,7 +409,7 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
         const variable_list saved = ctx->get_saved_variables();
         const at::Tensor &ids = saved[0], &w = saved[1], &nw = saved[2];
         const at::DeviceGuard guard(w.device());
-        const at::Tensor dy = grads[0].contiguous();
+        const at::Tensor dy = grads[0].resolve_neg().contiguous();
         const int64_t num = w.size(0), dim = w.size(1);
         const bool need_w = ctx->needs_input_grad(1), need_nw = ctx->needs_input_grad(2),
                    need_nb = ctx->needs_input_grad(3);

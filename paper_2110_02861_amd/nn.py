@@ -41,6 +41,7 @@ def _wants_grad(*tensors):
 
 def _packed_rows(x):
     """x as the kernels take it: packed, or a matrix of packed rows."""
+    x = x.resolve_neg()
     if x.is_contiguous() or (x.dim() == 2 and x.stride(1) == 1):
         return x
     return x.contiguous()
@@ -95,7 +96,7 @@ class _Embedding(torch.autograd.Function):
     def backward(ctx, dy):
         ids, = ctx.saved_tensors
         with _device_of(dy, "dy"):
-            dw = bq.bq_embedding_backward(dy.contiguous(), ids, *ctx.call)
+            dw = bq.bq_embedding_backward(dy.resolve_neg().contiguous(), ids, *ctx.call)
         return None, dw, None, None, None
 
 
@@ -132,7 +133,7 @@ class _StableEmbedding(torch.autograd.Function):
         need = ctx.needs_input_grad
         with _device_of(dy, "dy"):
             dweight, dw, db = bq.bq_stable_embedding_backward(
-                dy.contiguous(), ids, weight, norm_weight, *ctx.call,
+                dy.resolve_neg().contiguous(), ids, weight, norm_weight, *ctx.call,
                 need_norm=need[2] or need[3])
         return (None, dweight if need[1] else None, dw if need[2] else None,
                 db if need[3] else None, None, None, None)

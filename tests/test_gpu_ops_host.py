@@ -218,3 +218,27 @@ def test_clip_agrees(native, monkeypatch, handled):
     params[0].grad = normal((30, 80), 3)[:, ::2]
     with pytest.raises(ValueError):
         optim.clip_grad_norm_(params, 1.0)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_views_with_a_pending_negation(native, monkeypatch):
+    """Such views (the imaginary part of a conjugate is one) hold the values that they are
+    the negatives of."""
+    say("negated views", native)
+    if not native:
+        python_only(monkeypatch)
+    x, w, dy = normal((6, 40), 1), normal((40,), 2), normal((6, 40), 3)
+    table, ids = normal((10, 40), 4), torch.tensor([1, 2, 9, 1, 0, 1], device="cuda")
+    nx, ndy = torch._neg_view(x), torch._neg_view(dy)
+    assert nx.is_neg() and nx.is_contiguous()
+    assert torch.equal(nn.layer_norm(nx, w), nn.layer_norm(-x, w))
+    for run, leaf in ((lambda t: nn.layer_norm(t, w), x), (lambda t: nn.embedding(ids, t), table),
+                      (lambda t: nn.stable_embedding(ids, t), table)):
+        leaf = leaf.clone().requires_grad_()
+        a, = torch.autograd.grad(run(leaf), leaf, ndy)
+        b, = torch.autograd.grad(run(leaf), leaf, -dy)
+        assert torch.equal(a, b)
+    for bad in (lambda: bq.bq_layer_norm_forward(nx), lambda: nn.layer_norm(x, torch._neg_view(w)),
+                lambda: nn.embedding(ids, torch._neg_view(table)), lambda: bq.bq_grad_norm([nx])):
+        with pytest.raises(TypeError, match="negation"):
+            bad()
