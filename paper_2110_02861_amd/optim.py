@@ -606,8 +606,8 @@ def grad_norm(parameters, norm_type: float = 2.0) -> torch.Tensor:
 def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
                     error_if_nonfinite: bool = False) -> torch.Tensor:
     """torch.nn.utils.clip_grad_norm_ in HIP kernels: gradients times min(1, max_norm /
-    (norm + 1e-6)) in place; returns the norm from before (``grad_norm``).  Where the norm
-    is within max_norm the gradients are only read.  The host waits for nothing, so the
+    (norm + 1e-6)) in place; returns the norm from before (``grad_norm``).  Gradients must
+    not overlap in memory.  Where the norm is within max_norm they are only read.  The host waits for nothing, so the
     call can be captured into a graph, unless error_if_nonfinite asks for a RuntimeError
     (with the gradients unchanged) on a norm that is not finite."""
     if not max_norm >= 0.0:
