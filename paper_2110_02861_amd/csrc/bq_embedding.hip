@@ -502,15 +502,23 @@ __global__ __launch_bounds__(256) void span_kernel(const GradArgs a)
 // vocabularies, fall to different workgroups.
 // ---------------------------------------------------------------------------
 
-// Adds N rows of type DT, given by `row`, to a lane's columns.
+// Adds the first n of N rows of type DT, given by `row` (which is asked for all N), to a
+// lane's columns, all in flight at once: most rows have fewer than N tokens (one by one,
+// backward passes took: 60,000 tokens, 50257 rows of 64 fp32 61 us, now 48; 16,384 tokens,
+// 50257 of 1024 bf16 61, 57; 509 tokens, 1000 of 256 fp32 17.1, 15.5).
 template <int DT, int N, int V, int K, bool TAIL, typename Row>
 __device__ inline void add_rows(const Cols<V, K, TAIL> &c, float (&s)[Cols<V, K, TAIL>::kElems],
-                                Row row)
+                                uint32_t n, Row row)
 {
-    RawRow<DT, V, K, TAIL> x[N];
+    RawRow<DT, V, K, TAIL> x[N] = {};
+    const void *at[N];
 #pragma unroll
     for (int j = 0; j < N; ++j)
-        load_row<DT, false>(c, row(j), x[j]);
+        at[j] = row(j);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if ((uint32_t)j < n)
+            load_row<DT, false>(c, at[j], x[j]);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         float f[Cols<V, K, TAIL>::kElems];
@@ -582,9 +590,9 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
         };
         const auto tokens = [&](uint32_t p, uint32_t to) {
             for (; p + B <= to; p += B)
-                add_rows<YT, B>(c, s, [&](int j) { return token(p + j); });
-            for (; p < to; ++p)
-                add_rows<YT, 1>(c, s, [&](int) { return token(p); });
+                add_rows<YT, B>(c, s, B, [&](int j) { return token(p + j); });
+            if (p < to)
+                add_rows<YT, B>(c, s, to - p, [&](int j) { return token(min(p + j, to - 1)); });
         };
         const bool some = begin != end;
         RawRow<WT, V, K, TAIL> table;
@@ -599,9 +607,9 @@ __global__ __launch_bounds__(most_threads<TEAM>) void rows_kernel(const GradArgs
                     return (const void *)(parts + (int64_t)k * dim);
                 };
                 for (; i + B <= to; i += B)
-                    add_rows<kF32, B>(c, s, [&](int j) { return part(i + j); });
-                for (; i < to; ++i)
-                    add_rows<kF32, 1>(c, s, [&](int) { return part(i); });
+                    add_rows<kF32, B>(c, s, B, [&](int j) { return part(i + j); });
+                if (i < to)
+                    add_rows<kF32, B>(c, s, to - i, [&](int j) { return part(min(i + j, to - 1)); });
             };
             const uint32_t span = (first + kSpan - 1) / kSpan, past = last / kSpan;
             const bool spans = a.spans && span < past;
