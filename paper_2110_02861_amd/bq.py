@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 import warnings
 
 import numpy as np
@@ -657,9 +658,19 @@ def _dtype_id(t, name):
     return d
 
 
+def _eager():
+    """Refuses a call that a tracer records: the kernels write through addresses, so the
+    trace would hold the allocation of a result and nothing that fills it."""
+    import torch
+    fx = sys.modules.get("torch.fx.experimental.proxy_tensor")
+    if torch.jit.is_tracing() or (fx is not None and fx.get_proxy_mode() is not None):
+        raise NotImplementedError("libbq's kernels cannot be traced")
+
+
 def _on_device(t, name):
     """t, a dense GPU tensor on the current device."""
     import torch
+    _eager()
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided:
         raise TypeError(f"{name} must be a dense GPU torch tensor")
     if t.is_neg():
@@ -994,6 +1005,7 @@ def make_grad_array(grads):
 
 def _grad_norm(grads, norm_type, max_norm, out, workspace, stream):
     import torch
+    _eager()
     kind = _norm_kind(norm_type)
     grads = list(grads)
     arr = make_grad_array(grads)

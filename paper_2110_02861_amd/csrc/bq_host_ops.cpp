@@ -18,6 +18,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <ATen/TracerMode.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
@@ -50,11 +51,13 @@ struct Library {
 } lib;
 constexpr int kEntries = 12;
 
-// Calls that only the Python code goes through: Python modes, and torch.func's
-// transforms.
+// Calls that only the Python code goes through: Python modes, torch.func's transforms,
+// and tracing, which it refuses.
 bool modes()
 {
-    return c10::impl::TorchDispatchModeTLS::any_modes_set() ||
+    return at::tracer::impl::is_dispatch_enabled() ||
+           c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PreDispatch) ||
+           c10::impl::TorchDispatchModeTLS::any_modes_set() ||
            at::impl::PythonTorchFunctionTLS::stack_len() != 0 ||
            c10::impl::tls_local_dispatch_key_set().included_.has(
                c10::DispatchKey::FuncTorchDynamicLayerFrontMode);

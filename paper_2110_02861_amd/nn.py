@@ -5,7 +5,8 @@ Section 3.3, and the layer norm and embedding that it is made of, in HIP kernels
 libbq's kernels (``bq.bq_layer_norm_forward`` and its kin), ``LayerNorm`` and ``Embedding``
 the modules, with the parameters, names and initial values of torch's.  They take GPU
 tensors in fp32, fp16 or bf16 and raise for others: there is no CPU fallback.  Gradients
-are of first order, and the same bits every time.  A training step is captured into a graph
+are of first order, and the same bits every time.  Tracing (``torch.jit.trace``,
+``make_fx``) raises.  A training step is captured into a graph
 like one of torch's own layers: backward passes on a side stream, and no graph of an
 eager pass over the same leaves still alive.  ``StableEmbedding`` runs in plain torch
 unless it is built with ``fused=True``.
@@ -30,6 +31,7 @@ from . import bq
 
 def _device_of(t, name):
     """A context in which t's device is the current one."""
+    bq._eager()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a GPU torch tensor (libbq runs on the GPU only)")
     return torch.cuda.device(t.get_device())
