@@ -667,10 +667,22 @@ def _eager():
         raise NotImplementedError("libbq's kernels cannot be traced")
 
 
+def _no_tangent(*tensors):
+    """Refuses dual tensors of forward-mode differentiation: a result would come without a
+    tangent, as if it did not depend on them."""
+    import torch
+    from torch.autograd import forward_ad
+    if torch._C._is_fwd_grad_enabled():
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError("libbq's kernels have no forward-mode derivatives")
+
+
 def _on_device(t, name):
     """t, a dense GPU tensor on the current device."""
     import torch
     _eager()
+    _no_tangent(t)
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout is not torch.strided:
         raise TypeError(f"{name} must be a dense GPU torch tensor")
     if t.is_neg():
@@ -779,6 +791,7 @@ def bq_layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, stats: b
         if y is not None:
             return y
     import torch
+    _no_tangent(x, weight, bias)
     rows, cols, stride = _rows_of(x, "x")
     xt = _dtype_id(x, "x")
     pdtype, w, b = _norm_params(x, weight, bias, cols)
@@ -804,6 +817,7 @@ def bq_layer_norm_backward(dy, x, weight, mean, rstd, need_dx: bool = True,
     bq_layer_norm_forward returned them.  The parameters' gradients have weight's type
     (param_dtype where weight is None)."""
     import torch
+    _no_tangent(dy, x, weight, mean, rstd)
     rows, cols, stride = _rows_of(x, "x")
     xt = _dtype_id(x, "x")
     if not isinstance(dy, torch.Tensor) or dy.dtype != x.dtype or dy.shape != x.shape:
@@ -891,7 +905,7 @@ def bq_embedding_forward(weight, ids, scale: float = 1.0, out_dtype=None, out=No
 
 
 def _lookup_grad(dout, ids, dim):
-    import torch
+    _no_tangent(dout)
     ptr, bits = _ids_of(ids)
     _on_device(dout, "dout")
     if not dout.is_contiguous() or tuple(dout.shape) != (*ids.shape, dim):
@@ -929,6 +943,7 @@ def bq_stable_embedding_forward(weight, ids, norm_weight=None, norm_bias=None, e
                                     False)
         if y is not None:
             return y
+    _no_tangent(weight, norm_weight, norm_bias)
     wt, num, dim = _table_of(weight)
     ptr, bits = _ids_of(ids)
     dtype = _lookup_dtype(weight.dtype, out_dtype)
@@ -948,6 +963,7 @@ def bq_stable_embedding_backward(dout, ids, weight, norm_weight=None, eps: float
                                  stream=None):
     """(dweight, dnorm_weight, dnorm_bias) of the stable embedding, in weight's type; the
     last two None without need_norm."""
+    _no_tangent(dout, weight, norm_weight)
     wt, num, dim = _table_of(weight)
     ptr, bits, yt = _lookup_grad(dout, ids, dim)
     _lookup_dtype(weight.dtype, dout.dtype)

@@ -19,6 +19,7 @@
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/TracerMode.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
@@ -86,11 +87,18 @@ bq_dtype dtype_of(at::ScalarType t)
     return t == at::kFloat ? BQ_F32 : t == at::kHalf ? BQ_F16 : BQ_BF16;
 }
 
-// A dense tensor with memory of its own on the device.
+// Whether the tensor has a forward-mode tangent, which the kernels would drop.
+bool dual(const at::Tensor &t)
+{
+    return c10::AutogradState::get_tls_state().get_fw_grad_mode() &&
+           t._fw_grad(/*level=*/0).defined();
+}
+
+// A dense tensor with memory of its own on the device, and no tangent.
 const at::Tensor &dense(const at::Tensor &t, int device)
 {
     need(t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device &&
-         t.has_storage() && !t.is_neg() && !t.is_conj());
+         t.has_storage() && !t.is_neg() && !t.is_conj() && !dual(t));
     return t;
 }
 
@@ -145,6 +153,13 @@ bool wants_grad(std::initializer_list<const at::Tensor *> tensors)
 
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
+
+// What comes into a backward pass, as values in memory.
+at::Tensor incoming(const at::Tensor &dy)
+{
+    TORCH_CHECK_NOT_IMPLEMENTED(!dual(dy), "libbq's kernels have no forward-mode derivatives");
+    return dy.resolve_neg();
+}
 
 // Gradients of first order: as Python's once_differentiable, a second derivative raises.
 variable_list once(variable_list grads)
@@ -227,7 +242,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         const at::DeviceGuard guard(x.device());
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1),
                    need_b = ctx->needs_input_grad(2);
-        at::Tensor dy = grads[0].resolve_neg();
+        at::Tensor dy = incoming(grads[0]);
         if (!packed_rows(dy))
             dy = dy.contiguous();
         const auto pt = static_cast<at::ScalarType>(ctx->saved_data["param"].toInt());
@@ -320,7 +335,7 @@ struct Embedding : torch::autograd::Function<Embedding> {
     {
         const at::Tensor ids = ctx->get_saved_variables()[0];
         const at::DeviceGuard guard(ids.device());
-        const at::Tensor dy = grads[0].resolve_neg().contiguous();
+        const at::Tensor dy = incoming(grads[0]).contiguous();
         const int64_t num = ctx->saved_data["num"].toInt(), dim = dy.size(-1);
         const auto type = static_cast<at::ScalarType>(ctx->saved_data["dtype"].toInt());
         const auto scale = static_cast<float>(ctx->saved_data["scale"].toDouble());
@@ -412,7 +427,7 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
         const variable_list saved = ctx->get_saved_variables();
         const at::Tensor &ids = saved[0], &w = saved[1], &nw = saved[2];
         const at::DeviceGuard guard(w.device());
-        const at::Tensor dy = grads[0].resolve_neg().contiguous();
+        const at::Tensor dy = incoming(grads[0]).contiguous();
         const int64_t num = w.size(0), dim = w.size(1);
         const bool need_w = ctx->needs_input_grad(1), need_nw = ctx->needs_input_grad(2),
                    need_nb = ctx->needs_input_grad(3);

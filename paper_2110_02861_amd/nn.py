@@ -6,7 +6,7 @@ libbq's kernels (``bq.bq_layer_norm_forward`` and its kin), ``LayerNorm`` and ``
 the modules, with the parameters, names and initial values of torch's.  They take GPU
 tensors in fp32, fp16 or bf16 and raise for others: there is no CPU fallback.  Gradients
 are of first order, and the same bits every time.  Tracing (``torch.jit.trace``,
-``make_fx``) raises.  A training step is captured into a graph
+``make_fx``) and tensors with a forward-mode tangent raise.  A training step is captured into a graph
 like one of torch's own layers: backward passes on a side stream, and no graph of an
 eager pass over the same leaves still alive.  ``StableEmbedding`` runs in plain torch
 unless it is built with ``fused=True``.
@@ -77,6 +77,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     y = bq.host().layer_norm(x, weight, bias, eps, True)
     if y is not None:
         return y
+    bq._no_tangent(x, weight, bias)
     with _device_of(x, "x"):
         x = _packed_rows(x)
         if _wants_grad(x, weight, bias):
@@ -110,6 +111,7 @@ def embedding(ids, weight, padding_idx=None, scale: float = 1.0, out_dtype=None)
     y = bq.host().embedding(ids, weight, padding_idx, scale, out_dtype, True)
     if y is not None:
         return y
+    bq._no_tangent(weight)
     with _device_of(weight, "weight"):
         bq._padding(padding_idx, weight.size(0))
         ids = ids.contiguous()
@@ -151,6 +153,7 @@ def stable_embedding(ids, weight, norm_weight=None, norm_bias=None, eps: float =
                                    out_dtype, True)
     if y is not None:
         return y
+    bq._no_tangent(weight, norm_weight, norm_bias)
     with _device_of(weight, "weight"):
         bq._padding(padding_idx, weight.size(0))
         ids = ids.contiguous()
