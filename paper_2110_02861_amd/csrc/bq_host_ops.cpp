@@ -161,6 +161,26 @@ at::Tensor incoming(const at::Tensor &dy)
     return dy.resolve_neg();
 }
 
+// A tensor that the forward pass saved, packed.  Hooks on saved tensors (as of
+// torch.autograd.graph.saved_tensors_hooks) may hand back another one than they were
+// given: what the kernels read through its address is checked again.
+at::Tensor saved_as(const at::Tensor &t, at::IntArrayRef sizes, at::ScalarType type,
+                    at::Device device)
+{
+    if (!t.defined())
+        return t;
+    TORCH_CHECK(t.layout() == at::kStrided && t.device() == device && t.scalar_type() == type &&
+                    t.sizes() == sizes,
+                "a saved tensor came back on another device, or of another type or shape");
+    return t.resolve_neg().contiguous();
+}
+
+// Saved token ids.
+at::Tensor saved_ids(const at::Tensor &t, at::IntArrayRef sizes, at::Device device)
+{
+    return saved_as(t, sizes, t.scalar_type() == at::kInt ? at::kInt : at::kLong, device);
+}
+
 // Gradients of first order: as Python's once_differentiable, a second derivative raises.
 variable_list once(variable_list grads)
 {
@@ -238,15 +258,23 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
         const variable_list saved = ctx->get_saved_variables();
-        const at::Tensor &x = saved[0], &w = saved[1];
-        const at::DeviceGuard guard(x.device());
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1),
                    need_b = ctx->needs_input_grad(2);
         at::Tensor dy = incoming(grads[0]);
+        const at::DeviceGuard guard(dy.device());
         if (!packed_rows(dy))
             dy = dy.contiguous();
         const auto pt = static_cast<at::ScalarType>(ctx->saved_data["param"].toInt());
-        const Rows r = rows_of(x), g = rows_of(dy);
+        const Rows g = rows_of(dy);
+        at::Tensor x = saved[0];
+        if (x.sizes() != dy.sizes() || x.scalar_type() != dy.scalar_type() ||
+            x.device() != dy.device() || x.layout() != at::kStrided || x.is_neg() ||
+            !packed_rows(x))
+            x = saved_as(x, dy.sizes(), dy.scalar_type(), dy.device());
+        const at::Tensor w = saved_as(saved[1], {g.cols}, pt, dy.device());
+        const at::Tensor mean = saved_as(saved[2], {g.rows}, at::kFloat, dy.device());
+        const at::Tensor rstd = saved_as(saved[3], {g.rows}, at::kFloat, dy.device());
+        const Rows r = rows_of(x);
         at::Tensor dx, dw, db, ws;
         if (need_x)
             dx = at::empty(x.sizes(), x.options());
@@ -259,8 +287,8 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
         }
         succeed(lib.norm_backward(dtype_of(x.scalar_type()), dtype_of(pt), data(dy), g.stride,
                                   data(x), r.stride, r.rows, r.cols, data(w),
-                                  static_cast<const float *>(data(saved[2])),
-                                  static_cast<const float *>(data(saved[3])), data(dx), data(dw),
+                                  static_cast<const float *>(data(mean)),
+                                  static_cast<const float *>(data(rstd)), data(dx), data(dw),
                                   data(db), data(ws), current(x)),
                 "bq_layer_norm_backward");
         return once({dx, dw, db, at::Tensor()});
@@ -333,9 +361,10 @@ struct Embedding : torch::autograd::Function<Embedding> {
 
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
-        const at::Tensor ids = ctx->get_saved_variables()[0];
-        const at::DeviceGuard guard(ids.device());
         const at::Tensor dy = incoming(grads[0]).contiguous();
+        const at::DeviceGuard guard(dy.device());
+        const at::Tensor ids = saved_ids(ctx->get_saved_variables()[0],
+                                         dy.sizes().slice(0, dy.dim() - 1), dy.device());
         const int64_t num = ctx->saved_data["num"].toInt(), dim = dy.size(-1);
         const auto type = static_cast<at::ScalarType>(ctx->saved_data["dtype"].toInt());
         const auto scale = static_cast<float>(ctx->saved_data["scale"].toDouble());
@@ -417,6 +446,8 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
     {
         at::Tensor y = stable_forward(ids, w, nw, nb, eps, static_cast<at::ScalarType>(out));
         ctx->save_for_backward({ids, w, nw});
+        ctx->saved_data["num"] = w.size(0);
+        ctx->saved_data["dtype"] = static_cast<int64_t>(w.scalar_type());
         ctx->saved_data["eps"] = eps;
         ctx->saved_data["padding"] = padding;
         return y;
@@ -425,10 +456,14 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
         const variable_list saved = ctx->get_saved_variables();
-        const at::Tensor &ids = saved[0], &w = saved[1], &nw = saved[2];
-        const at::DeviceGuard guard(w.device());
         const at::Tensor dy = incoming(grads[0]).contiguous();
-        const int64_t num = w.size(0), dim = w.size(1);
+        const at::DeviceGuard guard(dy.device());
+        const int64_t num = ctx->saved_data["num"].toInt(), dim = dy.size(-1);
+        const auto type = static_cast<at::ScalarType>(ctx->saved_data["dtype"].toInt());
+        const at::Tensor ids =
+            saved_ids(saved[0], dy.sizes().slice(0, dy.dim() - 1), dy.device());
+        const at::Tensor w = saved_as(saved[1], {num, dim}, type, dy.device());
+        const at::Tensor nw = saved_as(saved[2], {dim}, type, dy.device());
         const bool need_w = ctx->needs_input_grad(1), need_nw = ctx->needs_input_grad(2),
                    need_nb = ctx->needs_input_grad(3);
         at::Tensor dw = at::empty({num, dim}, w.options()), dnw, dnb;

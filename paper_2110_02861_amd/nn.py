@@ -49,6 +49,10 @@ def _packed_rows(x):
     return x.contiguous()
 
 
+def _packed(t):
+    return None if t is None else t.resolve_neg().contiguous()
+
+
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
@@ -64,9 +68,10 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, mean, rstd = ctx.saved_tensors
         need_x, need_w, need_b, _ = ctx.needs_input_grad
         with _device_of(dy, "dy"):
+            # (hooks on saved tensors may hand them back in another order of memory)
             dx, dw, db = bq.bq_layer_norm_backward(
-                _packed_rows(dy), x, weight, mean, rstd, need_dx=need_x,
-                need_params=need_w or need_b, param_dtype=ctx.param_dtype)
+                _packed_rows(dy), _packed_rows(x), _packed(weight), _packed(mean), _packed(rstd),
+                need_dx=need_x, need_params=need_w or need_b, param_dtype=ctx.param_dtype)
         return dx, dw if need_w else None, db if need_b else None, None
 
 
@@ -99,7 +104,7 @@ class _Embedding(torch.autograd.Function):
     def backward(ctx, dy):
         ids, = ctx.saved_tensors
         with _device_of(dy, "dy"):
-            dw = bq.bq_embedding_backward(dy.resolve_neg().contiguous(), ids, *ctx.call)
+            dw = bq.bq_embedding_backward(_packed(dy), _packed(ids), *ctx.call)
         return None, dw, None, None, None
 
 
@@ -137,7 +142,7 @@ class _StableEmbedding(torch.autograd.Function):
         need = ctx.needs_input_grad
         with _device_of(dy, "dy"):
             dweight, dw, db = bq.bq_stable_embedding_backward(
-                dy.resolve_neg().contiguous(), ids, weight, norm_weight, *ctx.call,
+                _packed(dy), _packed(ids), _packed(weight), _packed(norm_weight), *ctx.call,
                 need_norm=need[2] or need[3])
         return (None, dweight if need[1] else None, dw if need[2] else None,
                 db if need[3] else None, None, None, None)
