@@ -94,11 +94,15 @@ bool dual(const at::Tensor &t)
            t._fw_grad(/*level=*/0).defined();
 }
 
+// Whether the tensor's elements are there: its storage may have been emptied (sharded
+// training does so), and a null parameter stands for ones or zeros in the C calls.
+bool in_memory(const at::Tensor &t) { return t.numel() == 0 || t.storage().data() != nullptr; }
+
 // A dense tensor with memory of its own on the device, and no tangent.
 const at::Tensor &dense(const at::Tensor &t, int device)
 {
     need(t.is_cuda() && t.layout() == at::kStrided && t.get_device() == device &&
-         t.has_storage() && !t.is_neg() && !t.is_conj() && !dual(t));
+         t.has_storage() && in_memory(t) && !t.is_neg() && !t.is_conj() && !dual(t));
     return t;
 }
 
@@ -161,18 +165,25 @@ at::Tensor incoming(const at::Tensor &dy)
     return dy.resolve_neg();
 }
 
-// A tensor that the forward pass saved, packed.  Hooks on saved tensors (as of
+// A tensor that the forward pass saved.  Hooks on saved tensors (as of
 // torch.autograd.graph.saved_tensors_hooks) may hand back another one than they were
-// given: what the kernels read through its address is checked again.
-at::Tensor saved_as(const at::Tensor &t, at::IntArrayRef sizes, at::ScalarType type,
-                    at::Device device)
+// given, and its memory may be gone: what the kernels read through its address is checked
+// again.
+at::Tensor checked(const at::Tensor &t, at::IntArrayRef sizes, at::ScalarType type,
+                   at::Device device)
 {
-    if (!t.defined())
-        return t;
     TORCH_CHECK(t.layout() == at::kStrided && t.device() == device && t.scalar_type() == type &&
                     t.sizes() == sizes,
                 "a saved tensor came back on another device, or of another type or shape");
-    return t.resolve_neg().contiguous();
+    TORCH_CHECK(in_memory(t), "a saved tensor has no memory any more");
+    return t.resolve_neg();
+}
+
+// The same packed; an undefined tensor as it is.
+at::Tensor saved_as(const at::Tensor &t, at::IntArrayRef sizes, at::ScalarType type,
+                    at::Device device)
+{
+    return t.defined() ? checked(t, sizes, type, device).contiguous() : t;
 }
 
 // Saved token ids.
@@ -266,11 +277,9 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
             dy = dy.contiguous();
         const auto pt = static_cast<at::ScalarType>(ctx->saved_data["param"].toInt());
         const Rows g = rows_of(dy);
-        at::Tensor x = saved[0];
-        if (x.sizes() != dy.sizes() || x.scalar_type() != dy.scalar_type() ||
-            x.device() != dy.device() || x.layout() != at::kStrided || x.is_neg() ||
-            !packed_rows(x))
-            x = saved_as(x, dy.sizes(), dy.scalar_type(), dy.device());
+        at::Tensor x = checked(saved[0], dy.sizes(), dy.scalar_type(), dy.device());
+        if (!packed_rows(x))
+            x = x.contiguous();
         const at::Tensor w = saved_as(saved[1], {g.cols}, pt, dy.device());
         const at::Tensor mean = saved_as(saved[2], {g.rows}, at::kFloat, dy.device());
         const at::Tensor rstd = saved_as(saved[3], {g.rows}, at::kFloat, dy.device());
