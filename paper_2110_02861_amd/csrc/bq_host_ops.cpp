@@ -525,7 +525,8 @@ PyObject *stable_embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 bool one_range(const at::Tensor &t) { return t.is_contiguous() || t.is_non_overlapping_and_dense(); }
 
 // clip(list of parameters, max norm or None, kind) -> the norm of their gradients (clipped
-// in place unless max norm is None), or None
+// in place unless max norm is None), the status of a C call that failed (which must not be
+// made again: some of its launches may have run), or None
 PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     return handled([&]() -> PyObject * {
@@ -572,12 +573,12 @@ PyObject *clip(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             return clips ? lib.clip(list.data(), count, kind, max_norm, ws.data_ptr(), out, stream)
                          : lib.grad_norm(list.data(), count, kind, ws.data_ptr(), out, stream);
         });
-        succeed(status, "the gradient norm");
-        if (clips)
+        // (a call that failed on the GPU's side may have scaled some of them)
+        if (clips && (status == BQ_OK || status == BQ_ERR_HIP))
             for (const at::Tensor &g : grads)
                 if (!g.is_inference())
                     g.unsafeGetTensorImpl()->bump_version();
-        return THPVariable_Wrap(norm);
+        return status == BQ_OK ? THPVariable_Wrap(norm) : PyLong_FromLong(status);
     });
 }
 

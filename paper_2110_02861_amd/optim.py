@@ -600,6 +600,8 @@ def grad_norm(parameters, norm_type: float = 2.0) -> torch.Tensor:
     each dense in memory; squares are summed in fp64, in one order."""
     parameters = _list_of(parameters)
     norm = bq.host().clip(parameters, None, bq._norm_kind(norm_type))
+    if norm.__class__ is int:
+        bq._check(norm, "bq_grad_norm")
     return bq.bq_grad_norm(_grads_of(parameters), norm_type) if norm is None else norm
 
 
@@ -607,9 +609,9 @@ def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
                     error_if_nonfinite: bool = False) -> torch.Tensor:
     """torch.nn.utils.clip_grad_norm_ in HIP kernels: gradients times min(1, max_norm /
     (norm + 1e-6)) in place; returns the norm from before (``grad_norm``).  Gradients must
-    not overlap in memory.  Where the norm is within max_norm they are only read.  The host waits for nothing, so the
-    call can be captured into a graph, unless error_if_nonfinite asks for a RuntimeError
-    (with the gradients unchanged) on a norm that is not finite."""
+    not overlap in memory.  Where the norm is within max_norm they are only read.  The host
+    waits for nothing, so the call can be captured into a graph, unless error_if_nonfinite
+    asks for a RuntimeError (with the gradients unchanged) on a norm that is not finite."""
     if not max_norm >= 0.0:
         raise ValueError(f"invalid max_norm {max_norm}")
     parameters = _list_of(parameters)
@@ -618,10 +620,17 @@ def clip_grad_norm_(parameters, max_norm: float, norm_type: float = 2.0,
         if not torch.isfinite(norm):
             raise RuntimeError(f"the gradients' norm is {float(norm)}: they cannot be clipped")
     norm = bq.host().clip(parameters, max_norm, bq._norm_kind(norm_type))
+    if norm.__class__ is int:
+        bq._check(norm, "bq_clip_grad_norm")
     if norm is not None:
         return norm
     grads = _grads_of(parameters)
-    norm = bq.bq_clip_grad_norm(grads, max_norm, norm_type)
+    try:
+        norm = bq.bq_clip_grad_norm(grads, max_norm, norm_type)
+    except bq.BQError as e:
+        if e.status == bq.BQ_ERR_HIP:  # some of its launches may have run
+            torch.autograd.graph.increment_version(grads)
+        raise
     if grads:
         torch.autograd.graph.increment_version(grads)
     return norm
