@@ -710,7 +710,9 @@ Layout layout(int64_t count, int64_t num, int64_t dim, bool stable)
     l.spans = l.chunks + round_up(count / kChunk * dim * 4, 256);
     l.partials = l.spans + (use_spans(count, num)
                                 ? round_up(count / (kChunk * kSpan) * dim * 4, 256) : 0);
-    l.bytes = l.partials + (stable ? stable_groups(dim) * 2 * dim * 4 : 0);
+    // of every workgroup, each with at least one row of the table
+    const int64_t groups = num < stable_groups(dim) ? num : stable_groups(dim);
+    l.bytes = l.partials + (stable ? groups * 2 * dim * 4 : 0);
     return l;
 }
 

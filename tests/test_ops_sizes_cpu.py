@@ -1,0 +1,18 @@
+"""Workspace sizes of the operators around the optimizer step: no more than a call can use."""
+from paper_2110_02861_amd import bq
+
+PARTIAL = 2 * 4  # bytes per column of the rows of partial sums: two gradients, fp32
+
+
+def test_stable_embedding_of_small_tables():
+    """A row of partial sums for every workgroup, of which there are no more than rows of
+    the table."""
+    lib = bq.lib()
+    for num, dim in ((1, 16384), (97, 9000), (1000, 2000), (2, 8)):
+        for count in (0, 1, 500):
+            rest = lib.bq_embedding_workspace_bytes(count, num, dim)
+            assert rest + num * dim * PARTIAL == \
+                lib.bq_stable_embedding_workspace_bytes(count, num, dim)
+    # large tables: as many as there are workgroups
+    rest = lib.bq_embedding_workspace_bytes(100, 50257, 1600)
+    assert lib.bq_stable_embedding_workspace_bytes(100, 50257, 1600) - rest == 1024 * 1600 * PARTIAL
