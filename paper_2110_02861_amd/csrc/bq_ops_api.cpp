@@ -96,7 +96,7 @@ bq_status bq_layer_norm_forward(bq_dtype dtype, bq_dtype param_dtype, const void
 
 int64_t bq_layer_norm_workspace_bytes(int64_t rows, int64_t cols)
 {
-    if (rows < 0 || cols < 1 || rows > kMaxRows || cols > kMaxCols)
+    if (check_norm(BQ_F32, BQ_F32, rows, cols, 0.0f) != BQ_OK)
         return 0;
     return bq::norm_workspace_bytes(rows, cols);
 }

@@ -1,4 +1,5 @@
-"""Workspace sizes of the operators around the optimizer step: no more than a call can use."""
+"""Workspace sizes of the operators around the optimizer step: no more than a call can
+use, and 0 where it refuses the sizes."""
 from paper_2110_02861_amd import bq
 
 PARTIAL = 2 * 4  # bytes per column of the rows of partial sums: two gradients, fp32
@@ -16,3 +17,12 @@ def test_stable_embedding_of_small_tables():
     # large tables: as many as there are workgroups
     rest = lib.bq_embedding_workspace_bytes(100, 50257, 1600)
     assert lib.bq_stable_embedding_workspace_bytes(100, 50257, 1600) - rest == 1024 * 1600 * PARTIAL
+
+def test_layer_norm_sizes_that_the_call_refuses():
+    lib = bq.lib()
+    for rows, cols in ((1 << 40, 1 << 27), (1 << 34, 1 << 27), ((1 << 40) + 1, 8),
+                       (8, (1 << 27) + 1)):
+        assert lib.bq_layer_norm_forward(bq.BQ_F32, bq.BQ_F32, 0x10000, rows, cols, cols, None, None,
+                                         1e-5, 0x10000, None, None, None) == bq.BQ_ERR_SIZE
+        assert lib.bq_layer_norm_workspace_bytes(rows, cols) == 0
+    assert lib.bq_layer_norm_workspace_bytes(1 << 33, 1 << 27) > 0
