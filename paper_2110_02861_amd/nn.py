@@ -168,6 +168,12 @@ def stable_embedding(ids, weight, norm_weight=None, norm_bias=None, eps: float =
         return bq.bq_stable_embedding_forward(weight, ids, norm_weight, norm_bias, eps, out_dtype)
 
 
+def _table_sizes(embeddings):
+    if embeddings.dim() != 2:
+        raise ValueError("embeddings must be a matrix")
+    return embeddings.shape
+
+
 class LayerNorm(torch.nn.LayerNorm):
     """torch.nn.LayerNorm over the last dimension, through ``layer_norm``: its parameters may
     be fp32 with inputs in fp16 or bf16."""
@@ -189,12 +195,21 @@ class Embedding(torch.nn.Embedding):
     dimension), in ``out_dtype``."""
 
     def __init__(self, num_embeddings: int, embedding_dim: int, padding_idx=None,
-                 scale: float = 1.0, out_dtype=None, device=None, dtype=None):
+                 scale: float = 1.0, out_dtype=None, device=None, dtype=None, *, _weight=None,
+                 _freeze: bool = False):
         if not math.isfinite(scale):
             raise ValueError(f"invalid scale {scale}")
-        super().__init__(num_embeddings, embedding_dim, padding_idx, device=device, dtype=dtype)
+        super().__init__(num_embeddings, embedding_dim, padding_idx, _weight=_weight,
+                         _freeze=_freeze, device=device, dtype=dtype)
         self.scale = float(scale)
         self.out_dtype = out_dtype
+
+    @classmethod
+    def from_pretrained(cls, embeddings, freeze: bool = True, padding_idx=None, *,
+                        scale: float = 1.0, out_dtype=None):
+        """A module around the table embeddings, which gets no gradient if freeze."""
+        return cls(*_table_sizes(embeddings), padding_idx, scale, out_dtype, _weight=embeddings,
+                   _freeze=freeze)
 
     def forward(self, input: torch.Tensor) -> torch.Tensor:
         return embedding(input, self.weight, self.padding_idx, self.scale, self.out_dtype)
@@ -209,7 +224,7 @@ class StableEmbedding(torch.nn.Embedding):
     def __init__(self, num_embeddings: int, embedding_dim: int, padding_idx=None,
                  max_norm=None, norm_type: float = 2.0, scale_grad_by_freq: bool = False,
                  sparse: bool = False, device=None, dtype=None, fused: bool = False,
-                 out_dtype=None):
+                 out_dtype=None, *, _weight=None, _freeze: bool = False):
         if sparse:
             raise ValueError("the 8-bit optimizers take dense gradients only")
         if fused and (max_norm is not None or scale_grad_by_freq):
@@ -217,11 +232,23 @@ class StableEmbedding(torch.nn.Embedding):
         if out_dtype is not None and not fused:
             raise ValueError("out_dtype needs fused=True")
         super().__init__(num_embeddings, embedding_dim, padding_idx, max_norm, norm_type,
-                         scale_grad_by_freq, sparse=False, device=device, dtype=dtype)
+                         scale_grad_by_freq, sparse=False, _weight=_weight, _freeze=_freeze,
+                         device=device, dtype=dtype)
+        if _weight is not None:
+            device, dtype = _weight.device, _weight.dtype
         self.norm = torch.nn.LayerNorm(embedding_dim, device=device, dtype=dtype)
         self.weight.bq_32bit_state = True
         self.fused = bool(fused)
         self.out_dtype = out_dtype
+
+    @classmethod
+    def from_pretrained(cls, embeddings, freeze: bool = True, padding_idx=None, max_norm=None,
+                        norm_type: float = 2.0, scale_grad_by_freq: bool = False,
+                        sparse: bool = False, *, fused: bool = False, out_dtype=None):
+        """A module around the table embeddings, which gets no gradient if freeze, with a layer
+        norm of its own."""
+        return cls(*_table_sizes(embeddings), padding_idx, max_norm, norm_type, scale_grad_by_freq,
+                   sparse, fused=fused, out_dtype=out_dtype, _weight=embeddings, _freeze=freeze)
 
     def reset_parameters(self) -> None:
         torch.nn.init.xavier_uniform_(self.weight)

@@ -1,0 +1,41 @@
+"""nn's modules on the CPU: tables taken over from elsewhere."""
+import pytest
+import torch
+import torch.nn.functional as F
+
+from paper_2110_02861_amd import nn
+
+
+def test_embedding_from_pretrained():
+    table = torch.randn(7, 5)
+    emb = nn.Embedding.from_pretrained(table)
+    assert type(emb) is nn.Embedding and emb.weight.data_ptr() == table.data_ptr()
+    assert (emb.num_embeddings, emb.embedding_dim, emb.padding_idx) == (7, 5, None)
+    assert not emb.weight.requires_grad and emb.scale == 1.0 and emb.out_dtype is None
+    emb = nn.Embedding.from_pretrained(table, freeze=False, padding_idx=-1, scale=2.0,
+                                       out_dtype=torch.float16)
+    assert emb.weight.requires_grad and emb.padding_idx == 6
+    assert emb.scale == 2.0 and emb.out_dtype == torch.float16
+    assert torch.equal(emb.weight, table)  # the padding row as it was given
+    with pytest.raises(TypeError):  # of torch's arguments, those that this module lacks
+        nn.Embedding.from_pretrained(table, max_norm=1.0)
+    with pytest.raises(ValueError):
+        nn.Embedding.from_pretrained(table[0])
+
+
+def test_stable_embedding_from_pretrained():
+    table = torch.randn(7, 5, dtype=torch.float64)
+    ids = torch.tensor([1, 6, 1])
+    emb = nn.StableEmbedding.from_pretrained(table, padding_idx=2)
+    assert type(emb) is nn.StableEmbedding and not emb.fused and emb.padding_idx == 2
+    assert emb.weight.data_ptr() == table.data_ptr() and not emb.weight.requires_grad
+    assert emb.weight.bq_32bit_state is True
+    assert emb.norm.weight.dtype == torch.float64 and emb.norm.weight.requires_grad
+    assert torch.equal(emb(ids), F.layer_norm(table[ids], (5,)))
+    emb = nn.StableEmbedding.from_pretrained(table.float(), freeze=False, fused=True,
+                                             out_dtype=torch.float16)
+    assert emb.fused and emb.out_dtype == torch.float16 and emb.weight.requires_grad
+    with pytest.raises(ValueError):
+        nn.StableEmbedding.from_pretrained(table, sparse=True)
+    with pytest.raises(ValueError):
+        nn.StableEmbedding.from_pretrained(table, fused=True, max_norm=1.0)
