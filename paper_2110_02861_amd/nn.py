@@ -215,9 +215,18 @@ class Embedding(torch.nn.Embedding):
         return embedding(input, self.weight, self.padding_idx, self.scale, self.out_dtype)
 
 
+def _called(norm):
+    """Whether a layer norm's module has to be called for what it does."""
+    return type(norm) not in (torch.nn.LayerNorm, LayerNorm) or bool(
+        norm._forward_hooks or norm._forward_pre_hooks or norm._backward_hooks or
+        norm._backward_pre_hooks)
+
+
 class StableEmbedding(torch.nn.Embedding):
     """fused=True runs lookup and layer norm as one HIP operator (``stable_embedding``), with
-    results that differ from plain torch's by rounding; out_dtype is its result's type."""
+    results that differ from plain torch's by rounding; out_dtype is its result's type.  The
+    operator does not call the module ``norm``: where that has hooks, or is of another class
+    than a layer norm, the two run apart."""
 
     fused, out_dtype = False, None  # of modules saved before there was a choice
 
@@ -256,6 +265,9 @@ class StableEmbedding(torch.nn.Embedding):
 
     def forward(self, input: torch.Tensor) -> torch.Tensor:
         if self.fused:
+            if _called(self.norm):
+                y = self.norm(embedding(input, self.weight, self.padding_idx))
+                return y if self.out_dtype is None else y.to(self.out_dtype)
             return stable_embedding(input, self.weight, self.norm.weight, self.norm.bias,
                                     self.norm.eps, self.padding_idx, self.out_dtype)
         emb = F.embedding(input, self.weight, self.padding_idx, self.max_norm, self.norm_type,

@@ -1,4 +1,5 @@
-"""nn's modules on the CPU: tables taken over from elsewhere."""
+"""nn's modules on the CPU: tables taken over from elsewhere, and a layer norm with hooks
+inside of the fused stable embedding."""
 import pytest
 import torch
 import torch.nn.functional as F
@@ -39,3 +40,34 @@ def test_stable_embedding_from_pretrained():
         nn.StableEmbedding.from_pretrained(table, sparse=True)
     with pytest.raises(ValueError):
         nn.StableEmbedding.from_pretrained(table, fused=True, max_norm=1.0)
+
+def hooks(module):
+    """Ways to be called when the module is, each with its handle."""
+    yield module.register_forward_hook(lambda m, i, o: o + 1.0)
+    yield module.register_forward_pre_hook(lambda m, i: (i[0] * 2.0,))
+    yield module.register_full_backward_hook(lambda m, gi, go: None)
+    yield module.register_full_backward_pre_hook(lambda m, go: None)
+
+
+def test_fused_stable_embedding_calls_a_norm_that_has_hooks(monkeypatch):
+    """The two layers run apart then, the lookup by its own operator (torch's here)."""
+    emb = nn.StableEmbedding(10, 8, padding_idx=1, fused=True, out_dtype=torch.float16)
+    plain = nn.StableEmbedding(10, 8, padding_idx=1)
+    plain.load_state_dict(emb.state_dict())
+    ids = torch.tensor([1, 2, 9])
+    fused = object()
+    monkeypatch.setattr(nn, "stable_embedding", lambda *a: fused)
+    monkeypatch.setattr(nn, "embedding",
+                        lambda i, w, padding_idx: F.embedding(i, w, padding_idx))
+    assert emb(ids) is fused
+    for h, g in zip(hooks(emb.norm), hooks(plain.norm)):
+        assert torch.equal(emb(ids), plain(ids).half())
+        h.remove()
+        g.remove()
+        assert emb(ids) is fused
+
+    class Other(torch.nn.LayerNorm):
+        def forward(self, x):
+            return super().forward(x) * 3.0
+    emb.norm = Other(8)
+    assert torch.equal(emb(ids), (F.layer_norm(F.embedding(ids, emb.weight), (8,)) * 3.0).half())
