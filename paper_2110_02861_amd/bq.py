@@ -690,8 +690,9 @@ def _on_device(t, name):
     if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{name} is on cuda:{t.get_device()}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
-    if t.numel() and t.untyped_storage().nbytes() == 0:
-        raise ValueError(f"{name} has no memory: its storage has been emptied")
+    # (a null pointer would stand for a parameter that was left out)
+    if t.numel() and (t.untyped_storage().nbytes() == 0 or t.data_ptr() == 0):
+        raise ValueError(f"{name} has no memory (an emptied storage, or a fake tensor)")
     return t
 
 

@@ -67,3 +67,24 @@ def test_emptied_before_the_backward_pass(which, half):
     empty(t[which])
     with pytest.raises((RuntimeError, ValueError), match="memory"):
         y.backward(torch.ones_like(y))
+
+
+@pytest.mark.filterwarnings("ignore:Accessing the data pointer")
+def test_tensors_without_memory_of_their_own(half):
+    """Fake tensors, and those that a transform wraps, have a null address."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    say("tensors without memory")
+    x, w, table = normal((4, 8), 1), normal((8,), 2), normal((10, 8), 3)
+    ids = torch.tensor([1, 2], device="cuda")
+    fake = FakeTensorMode().from_tensor(w)
+    calls = (lambda v: nn.layer_norm(x, v), lambda v: nn.layer_norm(x, w, v),
+             lambda v: bq.bq_layer_norm_forward(x, None, v),
+             lambda v: nn.stable_embedding(ids, table, v),
+             lambda v: nn.stable_embedding(ids, table, w, v))
+    for call in calls:
+        with pytest.raises(ValueError, match="memory"):
+            call(fake)
+        with pytest.raises(ValueError, match="memory"):
+            torch.func.functionalize(call)(w)
+    with FakeTensorMode() as mode, pytest.raises(ValueError, match="memory"):
+        nn.layer_norm(mode.from_tensor(x))
