@@ -25,6 +25,7 @@
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -74,6 +75,22 @@ auto unlocked(F f)
         ~Lock() { PyEval_RestoreThread(save); }
     } lock;
     return f();
+}
+
+// The tensor that f computes, without the interpreter lock.  An exception of Python code
+// that it ran (hooks on the tensors that it saved; checkpointing ends a recomputation by
+// one) is the call's, which is not made again.
+template <class F>
+PyObject *computed(F f)
+{
+    try {
+        return THPVariable_Wrap(unlocked(f));
+    } catch (python_error &e) {
+        e.restore();
+    } catch (pybind11::error_already_set &e) {
+        e.restore();
+    }
+    return PyErr_Occurred() ? nullptr : none();
 }
 
 void succeed(bq_status s, const char *what)
@@ -324,10 +341,10 @@ PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const at::Tensor b = vector(args[2], cols, pt, device);
         const double eps = real(args[3]);
         const bool grads = truth(args[4]) && wants_grad({&x, &w, &b});
-        return THPVariable_Wrap(unlocked([&] {
+        return computed([&] {
             return grads ? LayerNorm::apply(x, w, b, eps)
                          : norm_forward(x, w, b, eps, nullptr, nullptr);
-        }));
+        });
     });
 }
 
@@ -429,11 +446,11 @@ PyObject *embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const Lookup l = lookup_of(args[0], args[1], args[2], args[4], c10::hip::current_device());
         const double scale = real(args[3]);
         const bool grads = truth(args[5]) && wants_grad({&l.w});
-        return THPVariable_Wrap(unlocked([&] {
+        return computed([&] {
             return grads ? Embedding::apply(l.ids, l.w, l.padding, scale,
                                             static_cast<int64_t>(l.out))
                          : lookup_forward(l.ids, l.w, scale, l.out);
-        }));
+        });
     });
 }
 
@@ -509,11 +526,11 @@ PyObject *stable_embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const at::Tensor nb = vector(args[3], l.w.size(1), l.w.scalar_type(), device);
         const double eps = real(args[4]);
         const bool grads = truth(args[7]) && wants_grad({&l.w, &nw, &nb});
-        return THPVariable_Wrap(unlocked([&] {
+        return computed([&] {
             return grads ? StableEmbedding::apply(l.ids, l.w, nw, nb, eps, l.padding,
                                                   static_cast<int64_t>(l.out))
                          : stable_forward(l.ids, l.w, nw, nb, eps, l.out);
-        }));
+        });
     });
 }
 
