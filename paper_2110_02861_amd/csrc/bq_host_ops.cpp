@@ -13,6 +13,7 @@
 #include "bq_host.h"
 
 #include <cstring>
+#include <optional>
 #include <unordered_set>
 #include <vector>
 
@@ -175,6 +176,20 @@ bool wants_grad(std::initializer_list<const at::Tensor *> tensors)
 using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
 
+// A parameter as an argument of an autograd function: one that is left out is no tensor
+// (an undefined tensor may not be an input), and has no edge in the graph.
+using Param = std::optional<at::Tensor>;
+Param param(const at::Tensor &t) { return t.defined() ? Param(t) : std::nullopt; }
+at::Tensor given(const Param &p) { return p.has_value() ? *p : at::Tensor(); }
+
+// Whether the gradients of a weight and a bias are wanted, whose edges begin at `edge`.
+void wanted(AutogradContext *ctx, size_t edge, bool weight, bool &need_w, bool &need_b)
+{
+    const bool bias = ctx->saved_data["bias"].toBool();
+    need_w = weight && ctx->needs_input_grad(edge);
+    need_b = bias && ctx->needs_input_grad(edge + weight);
+}
+
 // What comes into a backward pass, as values in memory.
 at::Tensor incoming(const at::Tensor &dy)
 {
@@ -272,12 +287,14 @@ at::Tensor norm_forward(const at::Tensor &x, const at::Tensor &w, const at::Tens
 }
 
 struct LayerNorm : torch::autograd::Function<LayerNorm> {
-    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &x, const at::Tensor &w,
-                              const at::Tensor &b, double eps)
+    static at::Tensor forward(AutogradContext *ctx, const at::Tensor &x, const Param &weight,
+                              const Param &bias, double eps)
     {
+        const at::Tensor w = given(weight), b = given(bias);
         at::Tensor mean, rstd;
         at::Tensor y = norm_forward(x, w, b, eps, &mean, &rstd);
         ctx->save_for_backward({x, w, mean, rstd});
+        ctx->saved_data["bias"] = b.defined();
         ctx->saved_data["param"] = static_cast<int64_t>(
             w.defined() ? w.scalar_type() : b.defined() ? b.scalar_type() : x.scalar_type());
         return y;
@@ -286,8 +303,9 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
     static variable_list backward(AutogradContext *ctx, variable_list grads)
     {
         const variable_list saved = ctx->get_saved_variables();
-        const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1),
-                   need_b = ctx->needs_input_grad(2);
+        const bool need_x = ctx->needs_input_grad(0);
+        bool need_w, need_b;
+        wanted(ctx, 1, saved[1].defined(), need_w, need_b);
         at::Tensor dy = incoming(grads[0]);
         const at::DeviceGuard guard(dy.device());
         if (!packed_rows(dy))
@@ -342,7 +360,7 @@ PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const double eps = real(args[3]);
         const bool grads = truth(args[4]) && wants_grad({&x, &w, &b});
         return computed([&] {
-            return grads ? LayerNorm::apply(x, w, b, eps)
+            return grads ? LayerNorm::apply(x, param(w), param(b), eps)
                          : norm_forward(x, w, b, eps, nullptr, nullptr);
         });
     });
@@ -467,13 +485,15 @@ at::Tensor stable_forward(const at::Tensor &ids, const at::Tensor &w, const at::
 
 struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
     static at::Tensor forward(AutogradContext *ctx, const at::Tensor &ids, const at::Tensor &w,
-                              const at::Tensor &nw, const at::Tensor &nb, double eps,
+                              const Param &weight, const Param &bias, double eps,
                               int64_t padding, int64_t out)
     {
+        const at::Tensor nw = given(weight), nb = given(bias);
         at::Tensor y = stable_forward(ids, w, nw, nb, eps, static_cast<at::ScalarType>(out));
         ctx->save_for_backward({ids, w, nw});
         ctx->saved_data["num"] = w.size(0);
         ctx->saved_data["dtype"] = static_cast<int64_t>(w.scalar_type());
+        ctx->saved_data["bias"] = nb.defined();
         ctx->saved_data["eps"] = eps;
         ctx->saved_data["padding"] = padding;
         return y;
@@ -490,8 +510,9 @@ struct StableEmbedding : torch::autograd::Function<StableEmbedding> {
             saved_ids(saved[0], dy.sizes().slice(0, dy.dim() - 1), dy.device());
         const at::Tensor w = saved_as(saved[1], {num, dim}, type, dy.device());
         const at::Tensor nw = saved_as(saved[2], {dim}, type, dy.device());
-        const bool need_w = ctx->needs_input_grad(1), need_nw = ctx->needs_input_grad(2),
-                   need_nb = ctx->needs_input_grad(3);
+        const bool need_w = ctx->needs_input_grad(1);
+        bool need_nw, need_nb;
+        wanted(ctx, 2, nw.defined(), need_nw, need_nb);
         at::Tensor dw = at::empty({num, dim}, w.options()), dnw, dnb;
         if (need_nw)
             dnw = at::empty({dim}, w.options());
@@ -527,7 +548,7 @@ PyObject *stable_embedding(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         const double eps = real(args[4]);
         const bool grads = truth(args[7]) && wants_grad({&l.w, &nw, &nb});
         return computed([&] {
-            return grads ? StableEmbedding::apply(l.ids, l.w, nw, nb, eps, l.padding,
+            return grads ? StableEmbedding::apply(l.ids, l.w, param(nw), param(nb), eps, l.padding,
                                                   static_cast<int64_t>(l.out))
                          : stable_forward(l.ids, l.w, nw, nb, eps, l.out);
         });
