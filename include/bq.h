@@ -478,6 +478,8 @@ int64_t bq_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
  * Gradients of the layer norm: with g = dy * weight,
  *   dx = rstd (g - mean(g) - xh mean(g xh)),
  *   dweight = sum over rows of dy xh,  dbias = sum over rows of dy.
+ * xh is formed from the saved mean, which is rounded to fp32: far from zero it is off
+ * by up to 2^-24 |mean| rstd, where the forward pass's own is not.
  *   dy, x      device, rows rows, dy_stride and x_stride elements apart
  *   mean, rstd device, rows fp32 each, as bq_layer_norm_forward wrote them
  *   dx         device, rows x cols, packed (written), or NULL
@@ -606,7 +608,9 @@ bq_status bq_grad_norm(const bq_grad *grads, int32_t ngrads, bq_norm kind, void 
  * formed in fp64 and rounded to fp32; each product is rounded once to the
  * gradient's type.  Where c is 1 the gradients are left as they are.  The
  * gradients must not overlap (each would be multiplied more than once).  A norm
- * that is infinite makes c 0, a NaN makes it NaN, as IEEE arithmetic has it.
+ * that is infinite makes c 0, a NaN makes it NaN, as IEEE arithmetic has it; one
+ * above fp32's largest value is written as infinity, and c formed from its fp64
+ * value.  After BQ_ERR_HIP some gradients may be scaled: do not repeat the call.
  * The host reads nothing: the call can be captured into a graph.
  * Errors: as bq_grad_norm; BQ_ERR_ARG (max_norm negative or NaN).
  */

@@ -35,10 +35,14 @@ constexpr float kNaN = __builtin_nanf("");
 //   32768 x 1024 bf16 (128)          wave, 2: 27   4 waves, 1: 31   2: 28
 //   16384 x 4096 bf16 (512)          wave, 8: 61   4 waves, 2: 57   4: 54   8 waves, 1: 63
 //    4096 x 8192 bf16 (1024)         4 waves, 4: 29   8: 37         16 waves, 1: 43
-// A row's own wave needs no barrier; above 4 vectors per lane its registers cost more,
-// but not where rows are looked up (their loads take longer): 32768 tokens of 1600 fp32
-// (400 vectors)                       wave, 8: 72   4 waves, 2: 87   4: 70
-// and with the results streamed past the caches      56               86   63
+// A row's own wave needs no barrier; above 4 vectors per lane its registers cost more.
+// Looked-up rows of up to 512 vectors are a wave's with 8 all the same.  32768 tokens,
+// results streamed past the caches, calls that follow each other / behind a 1 GB fill
+// that flushes the memory-side cache:
+//   1600 fp32 (400 vectors)            wave, 8: 53 / 81   4 waves, 4: 50 / 72
+//   1300 fp32                                   45 / 69               43 / 62
+//   2000 fp32 to bf16                           49 / 77               47 / 69
+// On three tables in turn both take 58 with 1600 fp32.
 // ---------------------------------------------------------------------------
 
 template <int XT, int PT, int YT, bool GATHER, int TEAM, int K, int R, bool TAIL>
@@ -307,6 +311,15 @@ constexpr int64_t kNormGradGroups = 512;
 //   32768 x 1024 bf16  wave, 2: 44                                   53
 //    8192 x 4096 bf16  4 waves, 2: 49   4: 57   in 8 waves: 52
 //    4096 x 8192 bf16  4 waves, 4: 50           in 16 waves: 60
+// and above 1024 vectors, where a lane of 4 waves would hold 8:
+//    4096 x  8448 bf16  up to 16 waves, 2: 57   4 waves, 8: 91    up to 8 waves, 4: 244
+//    4096 x 12288 bf16                     88               106                     291
+//    2048 x 16384 bf16                     74               78                      178
+//    4096 x  4608 fp32                     54               48                      47
+//    4096 x  6144 fp32                     76               58                      64
+//    2048 x  8192 fp32                     63               46                      47
+// (16-bit rows need registers for 8 elements of a vector and spill; fp32 rows would gain by
+// fewer waves, and share the rule.)
 // ---------------------------------------------------------------------------
 
 template <int XT, int PT, int TEAM, int K, int R, bool TAIL>

@@ -177,9 +177,13 @@ __device__ inline void store_cols(void *p, int64_t c, int64_t n, const float (&v
 
 // Whether a lookup's results, of so many bytes, are stored with the non-temporal hint:
 // above what the L2 caches hold together (32 MB) they would push the table out of them
-// and of the memory-side cache.  Lookups of 1600 fp32, us, without / with: 4096 tokens
-// (26 MB) 9.6 / 8.7, 8192 17.3 / 14.6, 32768 72 / 56 (with the layer norm).  Whoever
-// reads them next loses 1 to 2 us by it, so short ones are stored as usual.
+// and of the memory-side cache.  Lookups of 1600 fp32 that follow each other, us, without
+// / with: 4096 tokens (26 MB) 9.6 / 8.7, 8192 17.3 / 14.6, 32768 56 / 47 (with the layer
+// norm 68 / 53; on three tables in turn 69 / 58).  Whoever reads them next loses 1 to 2 us
+// by it, so short ones are stored as usual.  Behind what flushes the memory-side cache (a
+// 1 GB fill here, the backward pass in training) the table's rows come from memory anyway
+// and the hint counts for little: 32768 69 / 66 (with the layer norm 83 / 81), 65536 to
+// bf16 96 / 103 (80 / 62 where they follow each other).
 __device__ inline bool stream_lookup(int64_t bytes) { return bytes > (int64_t{32} << 20); }
 
 // Byte address of row `row` of rows `stride` elements apart.
