@@ -216,17 +216,19 @@ class Embedding(torch.nn.Embedding):
 
 
 def _called(norm):
-    """Whether a layer norm's module has to be called for what it does."""
-    return type(norm) not in (torch.nn.LayerNorm, LayerNorm) or bool(
-        norm._forward_hooks or norm._forward_pre_hooks or norm._backward_hooks or
-        norm._backward_pre_hooks)
+    """Whether a layer norm's module has to be called for what it does (a class made for its
+    parametrized weight has torch's forward)."""
+    forward = getattr(type(norm), "forward", None)
+    return forward not in (torch.nn.LayerNorm.forward, LayerNorm.forward) or bool(
+        "forward" in norm.__dict__ or norm._forward_hooks or norm._forward_pre_hooks or
+        norm._backward_hooks or norm._backward_pre_hooks)
 
 
 class StableEmbedding(torch.nn.Embedding):
     """fused=True runs lookup and layer norm as one HIP operator (``stable_embedding``), with
     results that differ from plain torch's by rounding; out_dtype is its result's type.  The
-    operator does not call the module ``norm``: where that has hooks, or is of another class
-    than a layer norm, the two run apart."""
+    operator does not call the module ``norm``: where that has hooks, or another forward than
+    a layer norm's, the two run apart."""
 
     fused, out_dtype = False, None  # of modules saved before there was a choice
 

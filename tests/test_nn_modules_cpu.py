@@ -71,3 +71,23 @@ def test_fused_stable_embedding_calls_a_norm_that_has_hooks(monkeypatch):
             return super().forward(x) * 3.0
     emb.norm = Other(8)
     assert torch.equal(emb(ids), (F.layer_norm(F.embedding(ids, emb.weight), (8,)) * 3.0).half())
+
+
+def test_fused_stable_embedding_around_a_parametrized_norm(monkeypatch):
+    """The operator takes the parametrized weight; a module whose forward was replaced is
+    called."""
+    emb = nn.StableEmbedding(10, 8, fused=True)
+    seen = []
+    monkeypatch.setattr(nn, "stable_embedding", lambda *a: seen.append(a[2].detach()))
+    monkeypatch.setattr(nn, "embedding",
+                        lambda i, w, padding_idx: F.embedding(i, w, padding_idx))
+
+    class Double(torch.nn.Module):
+        def forward(self, w):
+            return w * 2.0
+    torch.nn.utils.parametrize.register_parametrization(emb.norm, "weight", Double())
+    emb(torch.tensor([1]))
+    assert torch.equal(seen[0], torch.full((8,), 2.0))
+    emb.norm.forward = lambda x: x + 1.0
+    ids = torch.tensor([1, 4])
+    assert torch.equal(emb(ids), emb.weight[ids] + 1.0) and len(seen) == 1
