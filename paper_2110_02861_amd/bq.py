@@ -724,7 +724,13 @@ def _vector(t, n, dtype, name):
 def _other(stream):
     """stream, where it is not the current one; else None."""
     import torch
-    return None if stream is None or stream == torch.cuda.current_stream() else stream
+    if stream is None:
+        return None
+    if stream.device_index != torch.cuda.current_device():
+        # the C calls run on the current device
+        raise ValueError(f"stream is on cuda:{stream.device_index}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return None if stream == torch.cuda.current_stream() else stream
 
 
 def _empty(shape, dtype, device, other):
